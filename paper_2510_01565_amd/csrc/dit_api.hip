@@ -695,6 +695,59 @@ dit_status noalloc_scratch(hipStream_t stream, void** out) {
   *out = table[dev];
   return DIT_OK;
 }
+// ---------------------------------------------------------------------------- 8-bit matrices
+constexpr int kFp8MaxK = 1 << 24;
+
+dit_status check_fp8_shape(int rows, int K, int block_rows) {
+  if (rows < 0 || K <= 0) return fail(DIT_ERR_INVALID_ARG, "rows %d K %d", rows, K);
+  if (block_rows != 1 && block_rows != kFp8Block)
+    return fail(DIT_ERR_INVALID_ARG, "block_rows %d must be 1 or %d", block_rows, kFp8Block);
+  if (K > kFp8MaxK) return fail(DIT_ERR_UNSUPPORTED, "K %d exceeds %d", K, kFp8MaxK);
+  return DIT_OK;
+}
+
+bool aligned_to(const void* p, int n) { return ((uintptr_t)p) % n == 0; }
+
+// ---------------------------------------------------------------------------- block-sparse attention
+SparseMeta make_sparse_meta(const dit_batch* b) {
+  SparseMeta m{};
+  m.n_req = b->n_req;
+  for (int r = 0; r < b->n_req; ++r) {
+    const int L = b->grid_h[r] * b->grid_w[r] + b->n_txt[r];
+    m.off[r + 1] = m.off[r] + L;
+    m.qb_off[r + 1] = m.qb_off[r] + (L + kSparseQ - 1) / kSparseQ;
+    m.kb_off[r + 1] = m.kb_off[r] + (L + kSparseK - 1) / kSparseK;
+    m.n_txt[r] = b->n_txt[r];
+  }
+  return m;
+}
+
+dit_status check_sparse(const dit_batch* batch, int heads, int head_dim, int dtype, SparseMeta* m) {
+  dit_status st;
+  if ((st = check_batch(batch, false))) return st;
+  if (dtype != DIT_F32 && dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "dtype %d", dtype);
+  if (heads <= 0 || head_dim <= 0) return fail(DIT_ERR_INVALID_ARG, "heads %d head_dim %d", heads, head_dim);
+  if ((dtype == DIT_BF16 && head_dim != 128 && head_dim != 64) || (dtype == DIT_F32 && head_dim != 64))
+    return fail(DIT_ERR_UNSUPPORTED, "head_dim %d with dtype %d", head_dim, dtype);
+  if (heads > 65535) return fail(DIT_ERR_UNSUPPORTED, "heads %d exceeds 65535", heads);
+  *m = make_sparse_meta(batch);
+  for (int r = 0; r < m->n_req; ++r) {
+    const int n = m->kb_off[r + 1] - m->kb_off[r];
+    if (n > kSparseMaxKeyBlocks)
+      return fail(DIT_ERR_UNSUPPORTED, "request %d has %d key blocks, more than %d", r, n, kSparseMaxKeyBlocks);
+  }
+  return DIT_OK;
+}
+
+dit_status check_keep(int n_keep) {
+  if (n_keep < 1 || n_keep > kSparseMaxKeyBlocks)
+    return fail(DIT_ERR_INVALID_ARG, "n_keep %d outside [1, %d]", n_keep, kSparseMaxKeyBlocks);
+  return DIT_OK;
+}
+
+// bytes of the means of n blocks
+size_t means_bytes(int n, int heads, int head_dim) { return align256((size_t)n * heads * head_dim * sizeof(double)); }
+
 // Host validation of a dit_step call; fills the batch metadata and the
 // workspace bytes the step needs.  Enqueues nothing.
 dit_status check_step(const dit_config* cfg, const dit_weights* w, const dit_batch* batch, const void* latents,
@@ -1002,6 +1055,143 @@ dit_status dit_linear(int M, int N, int K, int dtype, const void* x, const void*
   p.g[0] = group(x, K, w, K, M, K, e);
   p.n_groups = 1;
   HIP_TRY(gemm((hipStream_t)stream, dtype, p));
+  return DIT_OK;
+}
+
+dit_status dit_fp8_layout(int rows, int K, int block_rows, size_t* code_bytes, size_t* scale_bytes) {
+  g_err.clear();
+  dit_status st;
+  if ((st = check_fp8_shape(rows, K, block_rows))) return st;
+  if (!code_bytes || !scale_bytes) return fail(DIT_ERR_INVALID_ARG, "code_bytes / scale_bytes is NULL");
+  *code_bytes = (size_t)rows * fp8_k_blocks(K) * kFp8Block;
+  *scale_bytes = ((size_t)rows + block_rows - 1) / block_rows * fp8_scale_pitch(K);
+  return DIT_OK;
+}
+
+dit_status dit_quantize_fp8(int rows, int K, int block_rows, int dtype, const void* x, void* codes, void* scales,
+                            void* stream) {
+  g_err.clear();
+  dit_status st;
+  if ((st = check_fp8_shape(rows, K, block_rows))) return st;
+  if (dtype != DIT_F32 && dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "dtype %d", dtype);
+  if (rows == 0) return DIT_OK;
+  if (!x || !codes || !scales) return fail(DIT_ERR_INVALID_ARG, "x / codes / scales is NULL");
+  if (!aligned_to(x, elem_size(dtype))) return fail(DIT_ERR_INVALID_ARG, "x is not aligned to its elements");
+  if (!aligned16(codes) || !aligned_to(scales, 4))
+    return fail(DIT_ERR_INVALID_ARG, "codes must be 16-byte and scales 4-byte aligned");
+  hipStream_t s = (hipStream_t)stream;
+  size_t cb = 0, sb = 0;
+  dit_fp8_layout(rows, K, block_rows, &cb, &sb);
+  const double bytes = (double)rows * K * elem_size(dtype) + (double)cb + (double)sb;
+  HIP_TRY(timed(s, "quantize_fp8", 0.0, bytes,
+                [&] { return launch_quantize_fp8(dtype, x, rows, K, block_rows, codes, scales, s); }));
+  return DIT_OK;
+}
+
+dit_status dit_linear_fp8(int M, int N, int K, const void* x_codes, const void* x_scales, const void* w_codes,
+                          const void* w_scales, const void* b, int b_dtype, void* y, int out_dtype, void* stream) {
+  g_err.clear();
+  dit_status st;
+  if (N <= 0) return fail(DIT_ERR_INVALID_ARG, "N %d", N);
+  if ((st = check_fp8_shape(M, K, 1))) return st;
+  if (out_dtype != DIT_F32 && out_dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "out_dtype %d", out_dtype);
+  if (b_dtype != DIT_F32 && b_dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "b_dtype %d", b_dtype);
+  if (M == 0) return DIT_OK;
+  if (!x_codes || !x_scales || !w_codes || !w_scales || !y)
+    return fail(DIT_ERR_INVALID_ARG, "x / w codes or scales or y is NULL");
+  if (!aligned16(x_codes) || !aligned16(w_codes) || !aligned_to(x_scales, 4) || !aligned_to(w_scales, 4))
+    return fail(DIT_ERR_INVALID_ARG, "codes must be 16-byte and scales 4-byte aligned");
+  if (!aligned_to(y, elem_size(out_dtype)) || (b && !aligned_to(b, elem_size(b_dtype))))
+    return fail(DIT_ERR_INVALID_ARG, "b / y is not aligned to its elements");
+  hipStream_t s = (hipStream_t)stream;
+  const double kp = (double)fp8_k_blocks(K) * kFp8Block;
+  const double bytes = ((double)M + N) * kp + (double)M * N * elem_size(out_dtype);
+  HIP_TRY(timed(s, "gemm_fp8", 2.0 * M * N * (double)K, bytes, [&] {
+    return launch_gemm_fp8(M, N, K, x_codes, x_scales, w_codes, w_scales, b, b_dtype, y, out_dtype, s);
+  }));
+  return DIT_OK;
+}
+
+dit_status dit_attention_query_blocks(const dit_batch* batch, int* n_blocks) {
+  g_err.clear();
+  dit_status st;
+  if ((st = check_batch(batch, false))) return st;
+  if (!n_blocks) return fail(DIT_ERR_INVALID_ARG, "n_blocks is NULL");
+  *n_blocks = make_sparse_meta(batch).qb_off[batch->n_req];
+  return DIT_OK;
+}
+
+dit_status dit_attention_select_workspace_size(const dit_batch* batch, int heads, int head_dim, int dtype, size_t* bytes) {
+  g_err.clear();
+  dit_status st;
+  SparseMeta m;
+  if ((st = check_sparse(batch, heads, head_dim, dtype, &m))) return st;
+  if (!bytes) return fail(DIT_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = means_bytes(m.qb_off[m.n_req], heads, head_dim) + means_bytes(m.kb_off[m.n_req], heads, head_dim);
+  return DIT_OK;
+}
+
+dit_status dit_attention_select(const dit_batch* batch, int heads, int head_dim, int dtype, const void* q, const void* k,
+                                int n_keep, int flags, int* blocks, void* ws, size_t ws_bytes, void* stream) {
+  g_err.clear();
+  dit_status st;
+  SparseMeta m;
+  if ((st = check_sparse(batch, heads, head_dim, dtype, &m))) return st;
+  if ((st = check_keep(n_keep))) return st;
+  if (flags & ~DIT_SELECT_TEXT) return fail(DIT_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
+  if (!q || !k || !blocks) return fail(DIT_ERR_INVALID_ARG, "q / k / blocks is NULL");
+  if (!aligned16(q) || !aligned16(k)) return fail(DIT_ERR_INVALID_ARG, "q / k must be 16-byte aligned");
+  if (!aligned_to(blocks, 4)) return fail(DIT_ERR_INVALID_ARG, "blocks must be 4-byte aligned");
+  const int nqb = m.qb_off[m.n_req], nkb = m.kb_off[m.n_req];
+  const size_t qb = means_bytes(nqb, heads, head_dim);
+  if ((st = check_ws(ws, ws_bytes, qb + means_bytes(nkb, heads, head_dim)))) return st;
+  double f = 0;
+  for (int r = 0; r < m.n_req; ++r)
+    f += 2.0 * (m.qb_off[r + 1] - m.qb_off[r]) * (m.kb_off[r + 1] - m.kb_off[r]) * heads * head_dim;
+  const double bytes = 2.0 * m.off[m.n_req] * heads * head_dim * elem_size(dtype) + 4.0 * heads * nqb * n_keep;
+  hipStream_t s = (hipStream_t)stream;
+  HIP_TRY(timed(s, "attention_select", f, bytes, [&] {
+    return launch_attention_select(dtype, q, k, heads, head_dim, m, flags & DIT_SELECT_TEXT, n_keep, (double*)ws,
+                                   (double*)((char*)ws + qb), blocks, s);
+  }));
+  return DIT_OK;
+}
+
+dit_status dit_attention_sparse_workspace_size(const dit_batch* batch, int heads, int head_dim, int dtype, size_t* bytes) {
+  g_err.clear();
+  dit_status st;
+  SparseMeta m;
+  if ((st = check_sparse(batch, heads, head_dim, dtype, &m))) return st;
+  if (!bytes) return fail(DIT_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = 0;
+  return DIT_OK;
+}
+
+dit_status dit_attention_sparse(const dit_batch* batch, int heads, int head_dim, int dtype, const void* q, const void* k,
+                                const void* v, const int* blocks, int n_keep, void* o, void* ws, size_t ws_bytes,
+                                void* stream) {
+  g_err.clear();
+  dit_status st;
+  SparseMeta m;
+  if ((st = check_sparse(batch, heads, head_dim, dtype, &m))) return st;
+  if ((st = check_keep(n_keep))) return st;
+  if (!q || !k || !v || !blocks || !o) return fail(DIT_ERR_INVALID_ARG, "q / k / v / blocks / o is NULL");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o))
+    return fail(DIT_ERR_INVALID_ARG, "q / k / v / o must be 16-byte aligned");
+  if (!aligned_to(blocks, 4)) return fail(DIT_ERR_INVALID_ARG, "blocks must be 4-byte aligned");
+  size_t need = 0;
+  dit_attention_sparse_workspace_size(batch, heads, head_dim, dtype, &need);
+  if (need && (st = check_ws(ws, ws_bytes, need))) return st;
+  double f = 0;
+  for (int r = 0; r < m.n_req; ++r) {
+    const double L = m.off[r + 1] - m.off[r];
+    f += 4.0 * L * fmin(L, (double)n_keep * kSparseK) * heads * head_dim;
+  }
+  const double bytes = 4.0 * m.off[m.n_req] * heads * head_dim * elem_size(dtype);
+  hipStream_t s = (hipStream_t)stream;
+  HIP_TRY(timed(s, "attention_sparse", f, bytes, [&] {
+    return launch_attention_sparse(dtype, q, k, v, blocks, n_keep, heads, head_dim, m, o, s);
+  }));
   return DIT_OK;
 }
 

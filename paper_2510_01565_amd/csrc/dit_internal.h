@@ -266,4 +266,34 @@ hipError_t launch_euler(int dtype, void* x, const void* v, int channels, const B
 hipError_t launch_v_transpose(int dtype, const void* v, const BatchMeta& meta, int heads, int d, void* vt,
                               hipStream_t s);
 
+// ----------------------------------------------------------------------------
+// 8-bit matrices.  Codes of a [rows, K] matrix: [rows][fp8_k_blocks(K) * 128],
+// zeros past K.  Scale bytes: [row blocks][fp8_scale_pitch(K)], 127 past the last
+// block of K.
+constexpr int kFp8Block = DIT_FP8_BLOCK;
+inline int fp8_k_blocks(int K) { return (K + kFp8Block - 1) / kFp8Block; }
+inline int fp8_scale_pitch(int K) { return (fp8_k_blocks(K) + 3) / 4 * 4; }
+
+hipError_t launch_quantize_fp8(int dtype, const void* x, long rows, int K, int block_rows, void* q, void* scales,
+                               hipStream_t s);
+hipError_t launch_gemm_fp8(int M, int N, int K, const void* x, const void* xs, const void* w, const void* ws,
+                           const void* bias, int bias_dtype, void* y, int out_dtype, hipStream_t s);
+
+// ----------------------------------------------------------------------------
+// Block-sparse attention: a packed batch in joint order, cut into query and key
+// blocks request by request.
+constexpr int kSparseQ = DIT_SPARSE_QUERIES, kSparseK = DIT_SPARSE_KEYS, kSparseMaxKeyBlocks = DIT_SPARSE_MAX_KEY_BLOCKS;
+struct SparseMeta {
+  int n_req;
+  int off[kMaxReq + 1];     // tokens
+  int qb_off[kMaxReq + 1];  // query blocks
+  int kb_off[kMaxReq + 1];  // key blocks
+  int n_txt[kMaxReq];
+};
+// qm, km: scratch for the means, heads * head_dim * (query blocks) and * (key blocks)
+hipError_t launch_attention_select(int dtype, const void* q, const void* k, int heads, int head_dim, const SparseMeta& m,
+                                   int text_first, int keep, double* qm, double* km, int* out, hipStream_t s);
+hipError_t launch_attention_sparse(int dtype, const void* q, const void* k, const void* v, const int* blocks, int keep,
+                                   int heads, int head_dim, const SparseMeta& m, void* o, hipStream_t s);
+
 }  // namespace dit

@@ -22,10 +22,15 @@ DIT_MAX_REQUESTS = 16
 DIT_MAX_GRID = 256
 DIT_FLAG_BATCH_INVARIANT = 1
 DIT_NOALLOC_SCRATCH_BYTES = 256 << 20
+DIT_FP8_BLOCK = 128
+DIT_SPARSE_QUERIES, DIT_SPARSE_KEYS, DIT_SPARSE_MAX_KEY_BLOCKS = 128, 64, 2048
+DIT_SELECT_TEXT = 1
 
 EXPORTED = ("dit_weight_count", "dit_weight_manifest", "dit_workspace_size", "dit_step", "dit_step_noalloc",
             "dit_block_forward", "euler_update", "dit_attention_workspace_size", "dit_attention", "dit_linear",
-            "dit_profile_start", "dit_profile_stop", "dit_profile_entry", "dit_last_error")
+            "dit_fp8_layout", "dit_quantize_fp8", "dit_linear_fp8", "dit_attention_query_blocks",
+            "dit_attention_select_workspace_size", "dit_attention_select", "dit_attention_sparse_workspace_size",
+            "dit_attention_sparse", "dit_profile_start", "dit_profile_stop", "dit_profile_entry", "dit_last_error")
 
 
 class DitError(RuntimeError):
@@ -80,6 +85,15 @@ def lib() -> ctypes.CDLL:
                                                    ctypes.POINTER(ctypes.c_size_t)]
         L.dit_attention.argtypes = [ctypes.POINTER(dit_batch), ip, ip, ip, vp, vp, vp, vp, vp, sz, vp]
         L.dit_linear.argtypes = [ip, ip, ip, ip, vp, vp, vp, vp, ip, vp]
+        bp, sp = ctypes.POINTER(dit_batch), ctypes.POINTER(ctypes.c_size_t)
+        L.dit_fp8_layout.argtypes = [ip, ip, ip, sp, sp]
+        L.dit_quantize_fp8.argtypes = [ip, ip, ip, ip, vp, vp, vp, vp]
+        L.dit_linear_fp8.argtypes = [ip, ip, ip, vp, vp, vp, vp, vp, ip, vp, ip, vp]
+        L.dit_attention_query_blocks.argtypes = [bp, ctypes.POINTER(ctypes.c_int)]
+        L.dit_attention_select_workspace_size.argtypes = [bp, ip, ip, ip, sp]
+        L.dit_attention_select.argtypes = [bp, ip, ip, ip, vp, vp, ip, ip, vp, vp, sz, vp]
+        L.dit_attention_sparse_workspace_size.argtypes = [bp, ip, ip, ip, sp]
+        L.dit_attention_sparse.argtypes = [bp, ip, ip, ip, vp, vp, vp, vp, ip, vp, vp, sz, vp]
         L.dit_profile_start.argtypes = []
         L.dit_profile_stop.argtypes = [ctypes.POINTER(ctypes.c_int)]
         L.dit_profile_entry.argtypes = [ip, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(ctypes.c_long),
@@ -207,6 +221,54 @@ def dit_attention(batch: Batch, heads: int, head_dim: int, dtype: int, q, k, v, 
 
 def dit_linear(M: int, N: int, K: int, dtype: int, x, w, b, y, out_dtype: int, stream=None) -> None:
     _check(lib().dit_linear(M, N, K, dtype, _ptr(x), _ptr(w), _ptr(b), _ptr(y), out_dtype, _stream(stream)))
+
+
+def fp8_layout(rows: int, K: int, block_rows: int) -> Tuple[int, int]:
+    """Bytes of the codes and of the scales of a [rows, K] 8-bit matrix."""
+    c, s = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(lib().dit_fp8_layout(rows, K, block_rows, ctypes.byref(c), ctypes.byref(s)))
+    return c.value, s.value
+
+
+def dit_quantize_fp8(rows: int, K: int, block_rows: int, dtype: int, x, codes, scales, stream=None) -> None:
+    _check(lib().dit_quantize_fp8(rows, K, block_rows, dtype, _ptr(x), _ptr(codes), _ptr(scales), _stream(stream)))
+
+
+def dit_linear_fp8(M: int, N: int, K: int, x_codes, x_scales, w_codes, w_scales, b, b_dtype: int, y, out_dtype: int,
+                   stream=None) -> None:
+    _check(lib().dit_linear_fp8(M, N, K, _ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), _ptr(b), b_dtype,
+                                _ptr(y), out_dtype, _stream(stream)))
+
+
+def attention_query_blocks(batch: Batch) -> int:
+    """Query blocks of all requests: the second dimension of the lists of a block-sparse attention."""
+    n = ctypes.c_int()
+    _check(lib().dit_attention_query_blocks(ctypes.byref(batch.c), ctypes.byref(n)))
+    return n.value
+
+
+def attention_select_workspace_size(batch: Batch, heads: int, head_dim: int, dtype: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().dit_attention_select_workspace_size(ctypes.byref(batch.c), heads, head_dim, dtype, ctypes.byref(n)))
+    return n.value
+
+
+def dit_attention_select(batch: Batch, heads: int, head_dim: int, dtype: int, q, k, n_keep: int, flags: int, blocks, ws,
+                         ws_bytes: int, stream=None) -> None:
+    _check(lib().dit_attention_select(ctypes.byref(batch.c), heads, head_dim, dtype, _ptr(q), _ptr(k), n_keep, flags,
+                                      _ptr(blocks), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def attention_sparse_workspace_size(batch: Batch, heads: int, head_dim: int, dtype: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().dit_attention_sparse_workspace_size(ctypes.byref(batch.c), heads, head_dim, dtype, ctypes.byref(n)))
+    return n.value
+
+
+def dit_attention_sparse(batch: Batch, heads: int, head_dim: int, dtype: int, q, k, v, blocks, n_keep: int, o, ws,
+                         ws_bytes: int, stream=None) -> None:
+    _check(lib().dit_attention_sparse(ctypes.byref(batch.c), heads, head_dim, dtype, _ptr(q), _ptr(k), _ptr(v),
+                                      _ptr(blocks), n_keep, _ptr(o), _ptr(ws), ws_bytes, _stream(stream)))
 
 
 def profile_start() -> None:

@@ -1,0 +1,192 @@
+"""Quantising to e4m3 and the products of 8-bit matrices on the GPU, against the
+fp64 reference.
+
+Tolerances.  Codes and scales: equal.  fp32 output: exact products summed in fp32,
+so an element is off by at most (K + 2) 2^-24 of the sum of its products'
+magnitudes (a rounding per addition, two for the bias).  bf16 output: half a step
+(2^-8 of the value), and of each 8 products the seven below the largest lose what
+lies under 2^-13 of it: 7 * 2^-13 of the products' magnitudes at most."""
+import numpy as np
+import pytest
+
+from oracle import lowbit_oracle as B
+from paper_2510_01565_amd import dit, synth
+from harness import to_dev
+
+pytestmark = pytest.mark.gpu
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _dt(name):
+    torch = _torch()
+    return (torch.bfloat16, dit.DIT_BF16) if name == "bf16" else (torch.float32, dit.DIT_F32)
+
+
+def _guarded(n):
+    """n bytes between two runs of 0xa5: the buffer and a check that nothing around it was written."""
+    torch = _torch()
+    t = torch.full((n + 512,), 0xa5, dtype=torch.uint8, device="cuda")
+    return t[256:256 + n], lambda: bool((t[:256] == 0xa5).all() and (t[256 + n:] == 0xa5).all())
+
+
+def _quantize(x, rows, K, block, dtype):
+    nc, ns = dit.fp8_layout(rows, K, block)
+    q, okq = _guarded(nc)
+    s, oks = _guarded(ns)
+    dit.dit_quantize_fp8(rows, K, block, dtype, x, q, s)
+    _torch().cuda.synchronize()
+    assert okq() and oks()
+    kb = -(-K // 128)
+    return q.cpu().numpy().reshape(rows, kb * 128), s.cpu().numpy().reshape(-(-rows // block), -(-kb // 4) * 4), q, s
+
+
+def _matrix(seed, rows, K, bf16):
+    """Normal values of widely differing rows and blocks, with zeros, an empty block and values far below their block's largest."""
+    x = synth.normal(seed, "x", (rows, K))
+    rng = np.random.default_rng(seed)
+    x *= np.exp(2 * rng.normal(size=(rows, 1))).astype(np.float32)
+    for j in range(0, K, 128):
+        x[:, j:j + 128] *= np.float32(2.0 ** rng.integers(-20, 20))
+    x[rng.random(x.shape) < 0.05] = 0
+    x[rng.random(x.shape) < 0.02] *= np.float32(2.0 ** -12)
+    if K > 256:
+        x[:, 128:256] = 0
+    t = _torch().from_numpy(x)
+    return t.to(_torch().bfloat16) if bf16 else t
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("rows,K", [(1, 1), (1, 128), (2, 129), (3, 7), (127, 512), (128, 513), (129, 640), (300, 1536), (5, 4100)])
+def test_quantize(rows, K, block, dtype):
+    x = _matrix(rows * 7 + K, rows, K, dtype == "bf16")
+    q, s, _, _ = _quantize(x.cuda(), rows, K, block, _dt(dtype)[1])
+    rq, rs = B.quantize_fp8(x.double().numpy(), block)
+    assert np.array_equal(s, rs)
+    assert np.array_equal(q, rq)
+
+
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("shift", [1, 3])
+@pytest.mark.parametrize("K", [64, 200])
+def test_quantize_unaligned_rows(shift, K, block):
+    """x anywhere its elements may lie: no 16-byte loads then."""
+    torch = _torch()
+    x = _matrix(K + shift, 40, K, True)
+    big = torch.zeros(40 * K + 8, dtype=torch.bfloat16, device="cuda")
+    big[shift:shift + 40 * K] = x.reshape(-1).cuda()
+    q, s, _, _ = _quantize(big[shift:], 40, K, block, dit.DIT_BF16)
+    rq, rs = B.quantize_fp8(x.double().numpy(), block)
+    assert np.array_equal(s, rs) and np.array_equal(q, rq)
+
+
+@pytest.mark.parametrize("block", [1, 128])
+def test_quantize_extreme_values(block):
+    """Infinities, NaN, the type's extremes and subnormals, a block of nothing finite, exact limits of a scale."""
+    torch = _torch()
+    x = torch.zeros((130, 300), dtype=torch.float32)
+    x[0, :6] = torch.tensor([float("inf"), -float("inf"), float("nan"), 1.0, -0.0, 3.0])
+    x[1, 128:256] = float("nan")
+    x[2, :3] = torch.tensor([3.4028234e38 / 2, 1e30, 1e-30])
+    x[3, :4] = torch.tensor([1e-45, -1e-45, 1.2e-38, 1e-41])
+    x[4, 128:132] = torch.tensor([448.0, 232.0, 1.0625, 1.1875])
+    x[5, 256:260] = torch.tensor([448.00003, 449.0, 2.0 ** -9, 1.0])
+    x[129, 299] = -1.75
+    q, s, _, _ = _quantize(x.cuda(), 130, 300, block, dit.DIT_F32)
+    rq, rs = B.quantize_fp8(x.double().numpy(), block)
+    assert np.array_equal(s, rs)
+    nan = (rq & 0x7f) == 0x7f
+    assert np.array_equal(nan, (q & 0x7f) == 0x7f)   # a NaN's sign is free
+    assert np.array_equal(q[~nan], rq[~nan])
+
+
+def _product(M, N, K, out, bias, seed, noise=None):
+    """Operands, the call's output, and the exact product with the sum of magnitudes."""
+    torch = _torch()
+    x = _matrix(seed, M, K, True)
+    w = torch.from_numpy(synth.normal(seed, "w", (N, K), std=0.02)).to(torch.bfloat16)
+    if noise is not None:
+        noise(x, w)
+    xq, xs, dxq, dxs = _quantize(x.cuda(), M, K, 1, dit.DIT_BF16)
+    wq, ws, dwq, dws = _quantize(w.cuda(), N, K, 128, dit.DIT_BF16)
+    b = None if bias is None else torch.from_numpy(synth.normal(seed, "b", (N,))).to(_dt(bias)[0])
+    y = torch.full((M * N + 8,), float("nan"), dtype=_dt(out)[0], device="cuda")
+    dit.dit_linear_fp8(M, N, K, dxq, dxs, dwq, dws, None if b is None else b.cuda(), _dt(bias or "bf16")[1], y, _dt(out)[1])
+    torch.cuda.synchronize()
+    assert torch.isnan(y[M * N:]).all()  # nothing behind the last row
+    xv, wv = B.dequantize_fp8(xq, xs, 1, K), B.dequantize_fp8(wq, ws, 128, K)
+    ref, mag = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
+    if b is not None:
+        ref, mag = ref + b.double().numpy(), mag + np.abs(b.double().numpy())
+    return y[:M * N].double().cpu().numpy().reshape(M, N), ref, mag
+
+
+def _check(got, ref, mag, K, out):
+    tol = (K + 2) * 2.0 ** -24 * mag
+    if out == "bf16":
+        tol += 2.0 ** -8 * np.abs(ref) + 7 * 2.0 ** -13 * mag
+    assert np.isfinite(got).all()
+    assert (np.abs(got - ref) <= tol).all(), (np.abs(got - ref) / tol).max()
+    # over the whole matrix the truncations and roundings do not add up: bf16's own rounding, fp32's a few steps
+    err = np.linalg.norm(got - ref) / np.linalg.norm(ref)
+    assert err < (2.0 ** -8 if out == "bf16" else 4 * K ** 0.5 * 2.0 ** -24), err
+
+
+SHAPES = [(1, 1, 1), (1, 3001, 64), (4, 9216, 384), (15, 33, 700), (16, 256, 128), (17, 100, 1536), (33, 1000, 250),
+          (64, 64, 6144), (65, 130, 129), (128, 128, 512), (129, 200, 640), (200, 511, 300), (333, 1024, 1536),
+          (577, 700, 1000), (1030, 2050, 390)]
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_linear_fp8(M, N, K, out):
+    bias = {0: None, 1: "bf16", 2: "f32"}[(M + N) % 3]
+    got, ref, mag = _product(M, N, K, out, bias, M + N + K)
+    _check(got, ref, mag, K, out)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [(2, 40, 300), (300, 300, 300)])
+def test_linear_fp8_nan_reaches_its_row_alone(M, N, K, out):
+    """A NaN or an infinity of x makes its own output row NaN, one of w its own column."""
+    def noise(x, w):
+        x[1, 5] = float("inf")
+        w[7, K - 1] = float("nan")
+    got, ref, _ = _product(M, N, K, out, "f32", 3, noise)
+    assert np.array_equal(np.isnan(got), np.isnan(ref))
+    assert np.isnan(ref).sum() == N + M - 1
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [3, 200])
+def test_linear_fp8_scales_of_every_size(M, out):
+    """Blocks whose scales lie 2^100 apart on either side, all powers passing through the same output."""
+    def noise(x, w):
+        for j in range(0, x.shape[1], 128):
+            e = (j // 128) * 11 - 50
+            x[:, j:j + 128] = (x[:, j:j + 128].float() * 2.0 ** e).to(x.dtype)
+            w[:, j:j + 128] = (w[:, j:j + 128].float() * 2.0 ** -e).to(w.dtype)
+    got, ref, mag = _product(M, 260, 1200, out, None, 5, noise)
+    _check(got, ref, mag, 1200, out)
+
+
+def test_linear_fp8_rows_do_not_depend_on_other_rows_values():
+    """Same M and N: a row's bits are its own, and equal on every call."""
+    torch = _torch()
+    M, N, K = 70, 300, 900
+    x = _matrix(1, M, K, True)
+    w = torch.from_numpy(synth.normal(1, "w", (N, K), std=0.02)).to(torch.bfloat16)
+    outs = []
+    for other in (0, 0, 1):
+        if other:
+            x[1:] = _matrix(2, M, K, True)[1:]
+        _, _, xq, xs = _quantize(x.cuda(), M, K, 1, dit.DIT_BF16)
+        _, _, wq, ws = _quantize(w.cuda(), N, K, 128, dit.DIT_BF16)
+        y = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+        dit.dit_linear_fp8(M, N, K, xq, xs, wq, ws, None, dit.DIT_BF16, y, dit.DIT_BF16)
+        outs.append(y.clone())
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0][0], outs[2][0]) and not torch.equal(outs[0], outs[2])
