@@ -1106,7 +1106,7 @@ dit_status dit_linear_fp8(int M, int N, int K, const void* x_codes, const void* 
   hipStream_t s = (hipStream_t)stream;
   const double kp = (double)fp8_k_blocks(K) * kFp8Block;
   const double bytes = ((double)M + N) * kp + (double)M * N * elem_size(out_dtype);
-  HIP_TRY(timed(s, "gemm_fp8", 2.0 * M * N * (double)K, bytes, [&] {
+  HIP_TRY(timed(s, gemm_fp8_config_name(M, N, K, out_dtype), 2.0 * M * N * (double)K, bytes, [&] {
     return launch_gemm_fp8(M, N, K, x_codes, x_scales, w_codes, w_scales, b, b_dtype, y, out_dtype, s);
   }));
   return DIT_OK;

@@ -278,6 +278,8 @@ hipError_t launch_quantize_fp8(int dtype, const void* x, long rows, int K, int b
                                hipStream_t s);
 hipError_t launch_gemm_fp8(int M, int N, int K, const void* x, const void* xs, const void* w, const void* ws,
                            const void* bias, int bias_dtype, void* y, int out_dtype, hipStream_t s);
+// name of the kernel launch_gemm_fp8 picks
+const char* gemm_fp8_config_name(int M, int N, int K, int out_dtype);
 
 // ----------------------------------------------------------------------------
 // Block-sparse attention: a packed batch in joint order, cut into query and key

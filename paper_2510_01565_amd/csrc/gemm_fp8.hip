@@ -19,7 +19,12 @@ namespace dit {
 
 namespace {
 
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
+
+struct Word {
+  int v;
+};
 
 struct Fp8Problem {
   const uint8_t* x;    // [M][Kp]
@@ -139,7 +144,367 @@ __global__ __launch_bounds__(256) void fp8_tile_kernel(const Fp8Problem p) {
   }
 }
 
+// ---------------------------------------------------------------- 256 x 256 tiles, bf16 output
+// s_waitcnt with vmcnt = n and the other counters left alone
+template <int n>
+__device__ __forceinline__ void wait_vmcnt() {
+  static_assert(n >= 0 && n < 64, "vmcnt");
+  __builtin_amdgcn_s_waitcnt((n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+// v, of an origin unknown to the compiler
+__device__ __forceinline__ int opaque(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+__device__ __forceinline__ void block_barrier() { asm volatile("s_barrier" ::: "memory"); }
+// c += 2^(sw + sx - 254) w x, the lowest byte of either scale word.  A volatile
+// statement: as a builtin the compiler moves it out of its turn between two
+// barriers.  It does not see what the statement is: nothing may write an operand
+// by vector arithmetic, nor read c, within the instruction's wait states.
+__device__ __forceinline__ void asm_mfma(f32x4_t& c, const i32x8_t& w, const i32x8_t& x, int sw, int sx) {
+  asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[0,0,0]"
+               : "+v"(c)
+               : "v"(w), "v"(x), "v"(sw), "v"(sx));
+}
+
+// grouped order: 8 M-tiles share each run of N-tiles, for L2 reuse of both operands
+__device__ __forceinline__ void tile_of(int id, int tm, int tn, int& im, int& in) {
+  constexpr int GM = 8;
+  const int grp = id / (GM * tn), first = grp * GM, size = min(tm - first, GM), in_grp = id - grp * GM * tn;
+  im = first + in_grp % size;
+  in = in_grp / size;
+}
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+struct __attribute__((packed, aligned(2))) Bf16x8 {
+  u32x4_t v;
+};
+__device__ __forceinline__ u32x4_t pack8(const float* v) {
+  return u32x4_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+}
+constexpr int kMaxBlocks256 = 256;  // of fp8_256_kernel: one per CU
+constexpr int kMinKTiles256 = 3;    // its loads run up to three K tiles ahead, into the next output tile at most
+
+// 8 waves, each 128 rows x 64 columns.  K tiles of 128 bytes (one scale block)
+// move by direct-to-LDS loads into two stages.  Two wave groups (waves 0-3 and
+// 4-7, one wave of each per SIMD) take turns: while one issues a cluster of 8
+// MFMAs, the other reads the fragments of its next cluster from LDS and issues
+// its share of the loads; block barriers hold the groups one turn apart.  A K
+// tile is 4 clusters: cluster c multiplies the wave's c-th quarter of X rows (2
+// fragments) with all its W rows (4 fragments, held for a whole tile, two tiles
+// in turn).  Read phase 4 kt + c takes the X of the next cluster, 4 kt + c + 1, and
+// part c of W of tile kt + 1, whose arrival its next phase waits for.  X's part c
+// of tile kt + 2 and W's of tile kt + 3 are loaded in phase 4 kt + c + 1; loads have
+// 5 phases until the wait that makes them visible.
+// A block works through its output tiles as one stream of K tiles: the loads of
+// the next output tile run ahead of the last K tiles of this one, and each
+// cluster's finished sums are written in its read phase of the next tile's first
+// K tile, beside the other group's MFMAs.
+// W's rows are dealt out to the fragments so that a lane holds 16 neighbouring
+// columns of a row: it writes 32 bytes straight from registers.
+__global__ __launch_bounds__(512) void fp8_256_kernel(const Fp8Problem p) {
+  constexpr int BM = 256, BN = 256, Q = 4;
+  constexpr int ROWB = 128, CPR = 8, RPI = 8;  // bytes and 16-byte chunks of a row, rows per wave load
+  constexpr int STAGE = BM * ROWB, SUB = STAGE / Q, REGION = 2 * STAGE;
+  static_assert(BM == BN, "one stage size");
+  // [X stage 0, 1 | W stage 0, 1 | scales stage 0, 1: 256 words of X, 4 copies of the words of W's two row blocks |
+  // bias of the last two output tiles]
+  constexpr int SCALES = 2 * REGION, SCALE_STAGE = 2048, BIAS = SCALES + 2 * SCALE_STAGE, BIAS_STAGE = 1024;
+  __shared__ uint4 lds[(BIAS + 2 * BIAS_STAGE) / 16];
+  char* const lbase = (char*)lds;
+  const int tn = (p.N + BN - 1) / BN, tm = (p.M + BM - 1) / BM, tiles = tm * tn;
+  // XCD x owns a contiguous range of tiles; its blocks take them in turn
+  const int xcd = blockIdx.x & 7, per = tiles >> 3, rem = tiles & 7;
+  const int tile_end = (xcd + 1) * per + min(xcd + 1, rem), tile_step = ((int)gridDim.x - xcd + 7) >> 3;
+  int tile_next = xcd * per + min(xcd, rem) + (blockIdx.x >> 3);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wv >> 2, wn = wv & 3;
+  // K tiles, and those of an output tile: an even number, the last one of zeros where K has an odd number
+  const int KT = p.kb, Kp = KT * kFp8Block, KE = (KT + 1) & ~1;
+  const int my_tiles = (tile_end - tile_next + tile_step - 1) / tile_step;
+
+  // LDS slot of chunk c of row r: 16 consecutive rows' chunks lie in 16 different 16-byte bank groups
+  auto swz = [](int row, int c) { return c ^ ((row >> 1) & 7); };
+  // byte offsets of this lane's row of a part; the part and the K tile travel in the scalar offset, which the
+  // range check counts
+  const int lrow = wv * RPI + lane / CPR, lc = swz(lrow, lane % CPR) * 16;
+  const int gx = (int)((uint32_t)(lrow / 32 * 128 + lrow % 32) * (uint32_t)Kp + lc);
+  const int gw = (int)((uint32_t)(lrow / 16 * 64 + lrow % 16 / 4 * 16 + lrow % 4) * (uint32_t)Kp + lc);
+  const int gs = (wv < 4 ? wv * 64 + lane : lane & 1) * p.pitch;
+  // Three streams of loads, X, W and scales, each at a K tile of an output tile of its own; a row that does not exist
+  // reads as zeros.
+  auto buffer = [](const uint8_t* base, int n) __attribute__((always_inline)) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, n, kBufferWord3);
+  };
+  // rows r0 .. r0 + most - 1 of n, as far as they exist.  The size is forced into a scalar register: left to itself the
+  // compiler holds it in a vector register and issues every load from a loop over the lanes' (equal) values.
+  auto rows = [&](const uint8_t* base, int r0, int most, int n, int pitch) __attribute__((always_inline)) {
+    return buffer(base + (long)r0 * pitch, __builtin_amdgcn_readfirstlane(max(min(n - r0, most), 0) * pitch));
+  };
+  auto tile_at = [&](int id, int& m0, int& n0) __attribute__((always_inline)) {
+    int im, in;
+    tile_of(id, tm, tn, im, in);
+    m0 = __builtin_amdgcn_readfirstlane(im * BM);
+    n0 = __builtin_amdgcn_readfirstlane(in * BN);
+  };
+  int m0, n0, m0_next, n0_next;  // this output tile and the next (behind the last one, itself again)
+  tile_at(tile_next, m0, n0);
+  m0_next = m0;
+  n0_next = n0;
+  int xm = m0, wn0 = n0, xk = 0, wk = 0;
+  auto load_x = [&](auto stc, auto cc) __attribute__((always_inline)) {  // part c
+    constexpr int st = decltype(stc)::value, c = decltype(cc)::value;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rows(p.x, xm, xk < KT ? BM : 0, p.M, Kp),
+        (__attribute__((address_space(3))) void*)(lbase + st * STAGE + c * SUB + wv * RPI * ROWB), 16, gx,
+        xk * ROWB + c * 32 * Kp, 0, 0);
+  };
+  auto load_w = [&](auto stc, auto cc) __attribute__((always_inline)) {
+    constexpr int st = decltype(stc)::value, c = decltype(cc)::value;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rows(p.w, wn0, wk < KT ? BN : 0, p.N, Kp),
+        (__attribute__((address_space(3))) void*)(lbase + REGION + st * STAGE + c * SUB + wv * RPI * ROWB), 16, gw,
+        wk * ROWB + c * 4 * Kp, 0, 0);
+  };
+  auto next_xk = [&]() __attribute__((always_inline)) {
+    const bool on = ++xk == KE;
+    xk = on ? 0 : xk;
+    xm = on ? m0_next : xm;
+  };
+  auto next_wk = [&]() __attribute__((always_inline)) {
+    const bool on = ++wk == KE;
+    wk = on ? 0 : wk;
+    wn0 = on ? n0_next : wn0;
+  };
+  // Scales: a word holds the bytes of 4 K tiles of a row, the first lowest.  The words of K tiles 4 g .. are read
+  // from LDS as they are needed; those of the next four are loaded while they are: X's by waves 0-3, a row per lane,
+  // W's by waves 4-7, each a copy.
+  auto load_scales = [&](int stage, int m, int n, int k) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t r = wv < 4 ? rows(p.xs, m, BM, p.M, p.pitch) : rows(p.ws, n >> 7, 2, (p.N + 127) >> 7, p.pitch);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        r, (__attribute__((address_space(3))) void*)(lbase + SCALES + stage * SCALE_STAGE + wv * 256), 4, gs, k, 0, 0);
+  };
+  // the tile's bias, one value per word, 64 of them by each of four waves (and again by the others); zeros past N
+  auto load_bias = [&](int stage) __attribute__((always_inline)) {
+    const int q = wv & 3, n = p.bias ? max(p.N - n0, 0) : 0, vo = q * 64 + lane;
+    __attribute__((address_space(3))) void* const to =
+        (__attribute__((address_space(3))) void*)(lbase + BIAS + stage * BIAS_STAGE + q * 256);
+    if (p.bias_f32)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer((const uint8_t*)p.bias + (long)n0 * 4, n * 4), to, 4, vo * 4, 0, 0, 0);
+    else
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer((const uint8_t*)p.bias + (long)n0 * 2, n * 2), to, 2, vo * 2, 0, 0, 0);
+  };
+
+  // ---- fragment reads: row lane % 16 of a 16-row fragment, chunks lane / 16 and lane / 16 + 4
+  const int xr = wm * 32 + (lane & 15), wr = wn * 16 + (lane & 15);
+  int xa[2], wa[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    xa[h] = xr * ROWB + swz(xr, (lane >> 4) + 4 * h) * 16;
+    wa[h] = REGION + wr * ROWB + swz(wr, (lane >> 4) + 4 * h) * 16;
+  }
+  // Whole-value casts: read member by member, the compiler takes them to alias the loads in flight and waits for those.
+  auto lds16 = [&](int at) __attribute__((always_inline)) {
+    return __builtin_bit_cast(i32x4_t, *(const uint4*)(lbase + at));
+  };
+  auto lds4 = [&](int at) __attribute__((always_inline)) {
+    return __builtin_bit_cast(int, *(const Word*)(lbase + at));
+  };
+  auto frag = [&](int lo, int hi) __attribute__((always_inline)) {
+    return __builtin_shufflevector(lds16(lo), lds16(hi), 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  const int xs0 = SCALES + (wm * 128 + (lane & 15)) * 4, ws0 = SCALES + 1024 + wv % 4 * 256 + (wn >> 1) * 4;
+  f32x4_t acc[8][4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  // X fragments of a cluster and its scale words (clusters in turn), W fragments of a K tile and its scale word (K tiles
+  // in turn)
+  i32x8_t fx[2][2], fw[2][4];
+  int sx[2][2], sw[2];
+  // reads part c of X of a K tile in `st` into the cluster's registers
+  auto read_x = [&](auto stc, auto cc, int stage) __attribute__((always_inline)) {
+    constexpr int st = decltype(stc)::value, c = decltype(cc)::value;
+    const int xsa = opaque(xs0 + stage * SCALE_STAGE);  // one address register, the rest in the reads' offsets
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      constexpr int off = st * STAGE + c * SUB;
+      fx[c & 1][i] = frag(xa[0] + off + i * 16 * ROWB, xa[1] + off + i * 16 * ROWB);
+      sx[c & 1][i] = lds4(xsa + (c * 32 + i * 16) * 4);
+    }
+    if constexpr (c == 0) sw[st] = lds4(opaque(ws0 + stage * SCALE_STAGE));
+  };
+
+  // ---- writes the finished sums of cluster c of the tile at (m0, n0), whose bias is in `stage`
+  const int ncol = wn * 64 + (lane >> 4) * 16, mrow = wm * 128 + (lane & 15);
+  const uint32_t pitch = (uint32_t)p.N * 2;
+  const int bias_shift = p.bias_f32 ? 0 : 16;
+  auto store = [&](auto cc, int m0, int n0, int stage) __attribute__((always_inline)) {
+    constexpr int c = decltype(cc)::value;
+    float b[16];
+    const int at = opaque(ncol) * 4 + BIAS + stage * BIAS_STAGE;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const i32x4_t v = lds16(at + q * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) b[q * 4 + e] = __uint_as_float((uint32_t)v[e] << bias_shift);
+    }
+    // opaque: what depends on the lane alone is formed here again rather than held in registers over the K loop
+    const int mr = opaque(mrow), n = p.N - n0 - opaque(ncol);  // n: columns left from this lane's first
+    const uint32_t yo = (uint32_t)mr * pitch + (uint32_t)(p.N - n0 - n) * 2;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float v[16];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[j * 4 + r] = acc[c * 2 + i][j][r] + b[j * 4 + r];
+      char* const y = (char*)p.y + ((long)m0 * p.N + n0) * 2 + (long)(c * 32 + i * 16) * pitch + yo;
+      if (mr < p.M - m0 - (c * 32 + i * 16)) {
+        if (n >= 16) {
+          ((Bf16x8*)y)->v = pack8(v);
+          ((Bf16x8*)(y + 16))->v = pack8(v + 8);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 15; ++e)
+            if (e < n) ((bf16_t*)y)[e] = f2bf(v[e]);
+        }
+      }
+    }
+  };
+
+  using S0 = std::integral_constant<int, 0>;
+  using S1 = std::integral_constant<int, 1>;
+  int prev_m0 = p.M, prev_n0 = 0, scale_stage = 0, bias_stage = 0;  // no row of the tile before the first exists
+  bool counted = false;
+  // STORE 1: the output tile's first K tile, which writes the previous tile's sums; 2: the one after it
+  auto phase = [&](auto stc, auto cc, auto storec, int kt) __attribute__((always_inline)) {
+    constexpr int st = decltype(stc)::value, c = decltype(cc)::value;
+    constexpr int STORE = decltype(storec)::value;
+    using CN = std::integral_constant<int, (c + 1) % Q>;
+    using SN = std::integral_constant<int, c + 1 < Q ? st : st ^ 1>;  // stage of the next cluster
+    using CP = std::integral_constant<int, (c + Q - 1) % Q>;
+    using SX = std::integral_constant<int, c == 0 ? st ^ 1 : st>;
+    using SW = std::integral_constant<int, c == 0 ? st : st ^ 1>;
+    if constexpr (STORE == 1) {
+      store(cc, prev_m0, prev_n0, bias_stage ^ 1);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          acc[c * 2 + i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+          asm volatile("" : "+v"(acc[c * 2 + i][j]));  // zeroed here, ahead of the barrier
+        }
+    }
+    // the last phase's reads, this cluster's operands among them; complete ahead of the barrier, after which their
+    // places may be loaded again
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    const int byte = (kt & 3) * 8;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) sx[c & 1][i] = opaque(opaque(sx[c & 1][i]) >> byte);
+    if constexpr (c == 0) sw[st] = opaque(opaque(sw[st]) >> byte);
+    // the next cluster's X; behind the last one of a K tile, whose scales may start another group
+    if (c + 1 == Q && st == 1 && (((kt + 1) & 3) == 0 || kt + 1 == KE)) scale_stage ^= 1;
+    read_x(SN{}, CN{}, scale_stage);
+    {
+      constexpr int off = (st ^ 1) * STAGE + c * SUB;
+      fw[st ^ 1][c] = frag(wa[0] + off, wa[1] + off);
+    }
+    // the last part of X's K tile kt + 1 and W's kt + 2, or a part of kt + 2 and kt + 3
+    load_x(SX{}, CP{});
+    load_w(SW{}, CP{});
+    if constexpr (c == 0) {
+      next_xk();
+      next_wk();
+    }
+    // All but the loads of the last 5 phases have landed.  Those phases' stores need not have: 4 in each phase of the
+    // first K tile, if all of the tile's rows and columns exist.
+    if (STORE && counted) wait_vmcnt<10 + (STORE == 1 ? 4 * (c + 1) : STORE == 2 ? 16 - 4 * c : 0)>();
+    else wait_vmcnt<10>();
+    block_barrier();
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) asm_mfma(acc[c * 2 + i][j], fw[st][j], fx[c & 1][i], sw[st], sx[c & 1][i]);
+    block_barrier();
+  };
+  // K tiles kt and kt + 1.  Scales come in groups of four K tiles, the last group of an output tile two or four: their
+  // loads have 8 phases or more.
+  auto k_pair = [&](auto firstc, int kt) __attribute__((always_inline)) {
+    constexpr int FIRST = decltype(firstc)::value;
+    if ((kt & 3) == 0) {
+      const bool on = kt + 4 >= KE;
+      load_scales(scale_stage ^ 1, on ? m0_next : m0, on ? n0_next : n0, on ? 0 : kt + 4);
+    }
+    static_for<Q>([&](auto cc) { phase(S0{}, cc, std::integral_constant<int, FIRST ? 1 : 0>{}, kt); });
+    static_for<Q>([&](auto cc) { phase(S1{}, cc, std::integral_constant<int, FIRST ? 2 : 0>{}, kt + 1); });
+  };
+  load_scales(0, m0, n0, 0);
+  static_for<Q>([&](auto cc) { load_w(S0{}, cc); });
+  next_wk();
+  static_for<Q>([&](auto cc) {
+    load_x(S0{}, cc);
+    load_w(S1{}, cc);
+  });
+  next_xk();
+  next_wk();
+  wait_vmcnt<Q * 2>();
+  block_barrier();
+  static_for<Q>([&](auto cc) {
+    constexpr int off = decltype(cc)::value * SUB;
+    fw[0][decltype(cc)::value] = frag(wa[0] + off, wa[1] + off);
+  });
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+  block_barrier();
+  static_for<Q - 1>([&](auto cc) {
+    load_x(S1{}, cc);
+    load_w(S0{}, cc);
+  });
+  wait_vmcnt<10>();  // X's first part and the scales among what landed
+  block_barrier();
+  read_x(S0{}, S0{}, 0);
+  if (wv >= 4) block_barrier();
+#pragma unroll 1
+  for (int t = 0; t < my_tiles; ++t) {
+    load_bias(bias_stage);
+    tile_next += tile_step;
+    if (tile_next < tile_end) tile_at(tile_next, m0_next, n0_next);
+    counted = prev_m0 + BM <= p.M && prev_n0 + BN <= p.N;  // 4 stores a phase by every wave
+    k_pair(std::true_type{}, 0);
+#pragma unroll 1
+    for (int kt = 2; kt < KE; kt += 2) k_pair(std::false_type{}, kt);
+    prev_m0 = m0;
+    prev_n0 = n0;
+    bias_stage ^= 1;
+    m0 = m0_next;
+    n0 = n0_next;
+  }
+  if (wv < 4) block_barrier();
+  wait_vmcnt<0>();  // the loads past the last K tile land before the block ends
+  asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");  // the last MFMAs' results
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(acc[i][j]));
+  static_for<Q>([&](auto cc) { store(cc, prev_m0, prev_n0, bias_stage ^ 1); });
+}
+
 }  // namespace
+
+// Which kernel a product takes.
+enum Fp8Cfg { FP8_TILE, FP8_256 };
+static Fp8Cfg pick(int M, int N, int K, int out_dtype) {
+  const long big = (long)((M + 255) / 256) * ((N + 255) / 256);
+  // offsets within a tile of 256 rows fit 32 bits up to 2^22 bytes a row
+  if (out_dtype == DIT_BF16 && fp8_k_blocks(K) >= kMinKTiles256 && K <= 1 << 22 && N <= 1 << 21 && big >= 64) return FP8_256;
+  return FP8_TILE;
+}
+
+const char* gemm_fp8_config_name(int M, int N, int K, int out_dtype) {
+  static const char* names[] = {"gemm_fp8_64x64", "gemm_fp8_256x256"};
+  return names[pick(M, N, K, out_dtype)];
+}
 
 hipError_t launch_gemm_fp8(int M, int N, int K, const void* x, const void* xs, const void* w, const void* ws,
                            const void* bias, int bias_dtype, void* y, int out_dtype, hipStream_t s) {
@@ -156,6 +521,12 @@ hipError_t launch_gemm_fp8(int M, int N, int K, const void* x, const void* xs, c
   p.N = N;
   p.kb = fp8_k_blocks(K);
   p.pitch = fp8_scale_pitch(K);
+  const Fp8Cfg cfg = pick(M, N, K, out_dtype);
+  if (cfg == FP8_256) {
+    const long big = (long)((M + 255) / 256) * ((N + 255) / 256);
+    hipLaunchKernelGGL(fp8_256_kernel, dim3((unsigned)std::min<long>(big, kMaxBlocks256)), dim3(512), 0, s, p);
+    return hipGetLastError();
+  }
   const long tiles = (long)((M + 63) / 64) * ((N + 63) / 64);
   if (out_dtype == DIT_F32)
     hipLaunchKernelGGL((fp8_tile_kernel<true>), grid_of(tiles), dim3(256), 0, s, p);

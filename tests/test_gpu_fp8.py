@@ -190,3 +190,63 @@ def test_linear_fp8_rows_do_not_depend_on_other_rows_values():
         dit.dit_linear_fp8(M, N, K, xq, xs, wq, ws, None, dit.DIT_BF16, y, dit.DIT_BF16)
         outs.append(y.clone())
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0][0], outs[2][0]) and not torch.equal(outs[0], outs[2])
+
+
+def _large(M, N, K, out, bias, seed, off=0):
+    """A product too large for the host: 64 bits on the GPU from the codes' values.  off: elements by which y is misaligned."""
+    torch = _torch()
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn((M, K), generator=gen, device="cuda") * torch.exp(torch.randn((M, 1), generator=gen, device="cuda"))
+    x *= torch.exp(2 * torch.randn((1, -(-K // 128)), generator=gen, device="cuda")).repeat_interleave(128, 1)[:, :K]
+    w = torch.randn((N, K), generator=gen, device="cuda") * 0.02
+    w *= torch.exp(torch.randn((-(-N // 128), 1), generator=gen, device="cuda")).repeat_interleave(128, 0)[:N]
+    ops = []
+    for t, block in ((x, 1), (w, 128)):
+        rows = t.shape[0]
+        nc, ns = dit.fp8_layout(rows, K, block)
+        q, s = torch.empty(nc, dtype=torch.uint8, device="cuda"), torch.empty(ns, dtype=torch.uint8, device="cuda")
+        dit.dit_quantize_fp8(rows, K, block, dit.DIT_F32, t.contiguous(), q, s)
+        kb = -(-K // 128)
+        v = q.view(torch.float8_e4m3fn).double().view(rows, kb, 128)
+        e = s.view(-1, -(-kb // 4) * 4)[:, :kb].long().repeat_interleave(block, 0)[:rows]
+        v = (v * ((e + 1023 - 127) << 52).view(torch.float64)[:, :, None]).view(rows, -1)[:, :K]
+        ops.append((q, s, v))
+    b = None if bias is None else torch.randn((N + 1,), generator=gen, device="cuda").to(_dt(bias)[0])[1:]
+    y = torch.full((off + M * N + 64,), 55.0, dtype=_dt(out)[0], device="cuda")
+    dit.profile_start()
+    dit.dit_linear_fp8(M, N, K, ops[0][0], ops[0][1], ops[1][0], ops[1][1], b, _dt(bias or "bf16")[1], y[off:], _dt(out)[1])
+    torch.cuda.synchronize()
+    ran = set(dit.profile_stop())
+    assert (y[:off] == 55).all() and (y[off + M * N:] == 55).all()
+    xv, wv = ops[0][2], ops[1][2]
+    ref, mag = xv @ wv.t().contiguous(), xv.abs() @ wv.abs().t().contiguous()
+    if b is not None:
+        ref += b.double()
+        mag += b.double().abs()
+    return y[off:off + M * N].view(M, N).double(), ref, mag, ran
+
+
+def _check_large(got, ref, mag, K, out):
+    torch = _torch()
+    tol = (K + 2) * 2.0 ** -24 * mag
+    if out == "bf16":
+        tol += 2.0 ** -8 * ref.abs() + 7 * 2.0 ** -13 * mag
+    assert torch.isfinite(got).all()
+    assert ((got - ref).abs() <= tol).all(), ((got - ref).abs() / tol).max()
+    err = ((got - ref).norm() / ref.norm()).item()
+    assert err < (2.0 ** -8 if out == "bf16" else 4 * K ** 0.5 * 2.0 ** -24), err
+
+
+@pytest.mark.parametrize("M,N,K,bias,off", [
+    (4099, 4111, 257, "bf16", 0),     # 17 x 17 tiles of 256 (one more than the blocks): K tiles 3, odd columns
+    (4099, 4104, 512, "f32", 0),      # 4
+    (4352, 4352, 600, None, 0),       # 5: the scales of the next tile are due one K tile after they are loaded
+    (4097, 4105, 700, "bf16", 1),     # 6, y on an odd element
+    (4100, 8200, 900, "f32", 3),      # 8, two to three tiles a block
+    (5000, 6001, 1100, "bf16", 0),    # 9
+    (2048, 2049, 1300, None, 5),      # 8 x 9 tiles, one a block
+])
+def test_linear_fp8_256x256(M, N, K, bias, off):
+    got, ref, mag, ran = _large(M, N, K, "bf16", bias, K, off)
+    assert "gemm_fp8_256x256" in ran, ran
+    _check_large(got, ref, mag, K, "bf16")
