@@ -162,29 +162,60 @@ struct SparseArgs {
 };
 
 // ---------------------------------------------------------------- bf16
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+
+// The running max is raised only when a tile's probabilities against it sum to
+// more than 2^8 in some lane: up to there fp32 and bf16 hold them as well as any.
+constexpr float kLazyMax = 256.0f;
+
+__device__ __forceinline__ void wait_vmcnt0_lgkmcnt0() { __builtin_amdgcn_s_waitcnt(7 << 4); }
+
+// N MFMAs, each after R LDS reads of its own: the reads of A MFMAs stay ahead
+template <int N, int R, int A>
+__device__ __forceinline__ void read_ahead() {
+  __builtin_amdgcn_sched_group_barrier(0x100, A * R, 0);
+  static_for<N - A>([&](auto) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+  });
+  __builtin_amdgcn_sched_group_barrier(0x008, A, 0);
+}
+
 // 4 waves x 32 queries.  S^T = K Q^T by v_mfma_f32_32x32x16_bf16: a lane holds
 // the scores of query lane % 32 for half of the keys, and its probabilities are
-// the B operand of O^T = V^T P^T.
+// the B operand of O^T = V^T P^T.  K and V blocks arrive as they lie in memory,
+// by direct-to-LDS loads into two stages, the next listed block's while this one
+// is worked on; V is transposed on its way from LDS to the matrix cores
+// (ds_read_b64_tr_b16: 16 lanes take a block of 4 keys x 16 dimensions, each lane
+// the 4 keys of one dimension), so no copy of V is made and the keys a lane gets
+// are those whose probabilities it holds.
 template <int HD>
-__global__ __launch_bounds__(256) void sparse_bf16_kernel(const SparseArgs a) {
-  constexpr int CH = HD / 8, KP = HD + 8;  // row pitch of the tiles in LDS
-  __shared__ uint4 ktile[kKB * KP / 8];
-  __shared__ bf16_t vtile[kKB * KP];
-  __shared__ uint32_t mask[kSparseMaxKeyBlocks / 32];
-  __shared__ uint16_t list[kSparseMaxKeyBlocks];
-  __shared__ int count;
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2)))
+void sparse_bf16_kernel(const SparseArgs a) {
+  constexpr int CH = HD / 8;           // 16-byte chunks of a row
+  constexpr int RPI = 64 / CH;         // rows per wave load
+  constexpr int NI = kKB / RPI / 4;    // loads of a tile per wave
+  constexpr int ROWB = HD * 2, TILE = kKB * ROWB, STAGE = 2 * TILE;
+  // [stage][K tile | V tile], then the list.  One array: with several the compiler waits for all loads ahead of every
+  // read of LDS.
+  constexpr int LIST = 2 * STAGE, MASK = LIST + kSparseMaxKeyBlocks * 2, COUNT = MASK + kSparseMaxKeyBlocks / 8;
+  __shared__ uint4 smem[COUNT / 16 + 1];
+  char* const lbase = (char*)smem;
+  uint16_t* const list = (uint16_t*)(lbase + LIST);
   const SparseMeta& m = a.meta;
   const int nqb = m.qb_off[m.n_req];
-  const int row = blockIdx.x, h = blockIdx.y;
+  // blocks of one XCD take consecutive units, head by head: its L2 holds their K and V
+  const int unit = xcd_remap(blockIdx.x, gridDim.x);
+  const int h = unit / nqb, row = unit - h * nqb;
   const int r = request_of(m.qb_off, m.n_req, row);
-  const int L = m.off[r + 1] - m.off[r], q0 = (row - m.qb_off[r]) * kQB;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hl = lane >> 5;
+  const int L = m.off[r + 1] - m.off[r], q0 = (row - m.qb_off[r]) * kQB, nkb = m.kb_off[r + 1] - m.kb_off[r];
+  const int tid = threadIdx.x, lane = tid & 63, hl = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const long tok = (long)a.heads * HD, base = (long)m.off[r] * tok + (long)h * HD;
   const bf16_t* Q = (const bf16_t*)a.q + base;
   const bf16_t* K = (const bf16_t*)a.k + base;
   const bf16_t* V = (const bf16_t*)a.v + base;
-  const int cnt = read_list(a.blocks + ((long)h * nqb + row) * a.keep, a.keep, m.kb_off[r + 1] - m.kb_off[r], mask, list,
-                            &count, tid, 256);
+
   const int qrow = q0 + wave * 32 + (lane & 31);
   bf16x8_t qf[HD / 16];
 #pragma unroll
@@ -193,66 +224,157 @@ __global__ __launch_bounds__(256) void sparse_bf16_kernel(const SparseArgs a) {
     if (qrow < L) u = *(const uint4*)(Q + qrow * tok + (s * 2 + hl) * 8);
     qf[s] = __builtin_bit_cast(bf16x8_t, u);
   }
-  f32x16_t o[HD / 32] = {};
-  float mx = -FLT_MAX, l = 0.f;
-  const float sl2 = a.scale * 1.4426950408889634f;
-  for (int t = 0; t < cnt; ++t) {
-    const int k0 = list[t] * kKB;
-    __syncthreads();
-    for (int i = tid; i < kKB * CH; i += 256) {
-      const int key = i / CH, c = i % CH;
-      uint4 ku = make_uint4(0, 0, 0, 0), vu = ku;
-      if (k0 + key < L) {
-        ku = *(const uint4*)(K + (k0 + key) * tok + c * 8);
-        vu = *(const uint4*)(V + (k0 + key) * tok + c * 8);
-      }
-      ktile[key * (KP / 8) + c] = ku;
-      *(uint4*)&vtile[key * KP + c * 8] = vu;
+  const int cnt = __builtin_amdgcn_readfirstlane(
+      read_list(a.blocks + ((long)h * nqb + row) * a.keep, a.keep, nkb, (uint32_t*)(lbase + MASK), list, (int*)(lbase + COUNT),
+                tid, 256));
+
+  // slot of chunk c of K row `key`: the 16 rows of a fragment read lie in 16 different 16-byte bank groups
+  auto kswz = [](int key, int c) { return HD == 128 ? c ^ (key & 15) : c ^ ((key >> 1) & 7); };
+  // of V row `key`: the 64-byte segments of 4 neighbouring rows lie in 4 different quarters of the banks
+  auto vswz = [](int key, int c) { return HD == 128 ? c ^ ((key & 3) << 2) : c ^ ((key & 2) << 1); };
+  int ko[NI], vo[NI];  // global byte offsets of this lane's loads inside a tile
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int key = (wave * NI + i) * RPI + lane / CH;
+    ko[i] = (key * (int)tok + kswz(key, lane % CH) * 8) * 2;
+    vo[i] = (key * (int)tok + vswz(key, lane % CH) * 8) * 2;
+  }
+  auto tile_load = [&](int b, auto stc) __attribute__((always_inline)) {
+    constexpr int st = decltype(stc)::value;
+    const int k0 = b * kKB;
+    const int bytes = ((min(L - k0, kKB) - 1) * (int)tok + HD) * 2;  // keys past L read as zeros
+    const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(K + k0 * tok), (short)0, bytes, kBufferWord3);
+    const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(V + k0 * tok), (short)0, bytes, kBufferWord3);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int o = ko[i];
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rk, (__attribute__((address_space(3))) void*)(lbase + st * STAGE + (wave * NI + i) * 1024), 16, o, 0, 0, 0);
     }
-    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int o = vo[i];
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rv, (__attribute__((address_space(3))) void*)(lbase + st * STAGE + TILE + (wave * NI + i) * 1024), 16, o, 0, 0, 0);
+    }
+  };
+  auto block_at = [&](int i) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane((int)list[i]); };
+  using S0 = std::integral_constant<int, 0>;
+  using S1 = std::integral_constant<int, 1>;
+  if (cnt > 0) tile_load(block_at(0), S0{});
+
+  f32x16_t o[HD / 32] = {};
+  float mx = -FLT_MAX, l = 0.f;  // a finite start: keys whose scores are all -inf add nothing
+  const float sl2 = a.scale * 1.4426950408889634f;
+  // LDS byte offsets of this lane's fragment reads: K row lane % 32, chunk 2 ks + hl; V rows hl * 4 + lane % 16 / 4,
+  // dimensions 32 db + lane / 16 % 2 * 16 + lane % 4 * 4
+  int kf[HD / 16], vf[HD / 32];
+#pragma unroll
+  for (int ks = 0; ks < HD / 16; ++ks) kf[ks] = (lane & 31) * ROWB + kswz(lane & 31, ks * 2 + hl) * 16;
+#pragma unroll
+  for (int db = 0; db < HD / 32; ++db) {
+    const int key = hl * 4 + (lane & 15) / 4;
+    vf[db] = TILE + key * ROWB + vswz(key, db * 4 + (lane >> 4 & 1) * 2 + (lane & 3) / 2) * 16 + (lane & 1) * 8;
+  }
+  auto step = [&](int b, int next, auto stc, auto maskc) __attribute__((always_inline)) {
+    constexpr int st = decltype(stc)::value;
+    if (next >= 0) tile_load(next, std::integral_constant<int, st ^ 1>{});
     f32x16_t s[2] = {};
 #pragma unroll
     for (int ks = 0; ks < HD / 16; ++ks)
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, ktile[(b * 32 + (lane & 31)) * (KP / 8) + ks * 2 + hl]);
-        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s[b], 0, 0, 0);
+      for (int kb = 0; kb < 2; ++kb) {
+        const bf16x8_t u = __builtin_bit_cast(bf16x8_t, *(const uint4*)(lbase + kf[ks] + st * STAGE + kb * 32 * ROWB));
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(u, qf[ks], s[kb], 0, 0, 0);
       }
-    float tm = mx;
+    read_ahead<2 * HD / 16, 1, 4>();
+    if constexpr (decltype(maskc)::value) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = k0 + b * 32 + (i >> 2) * 8 + hl * 4 + (i & 3);
-        s[b][i] = key < L ? s[b][i] * sl2 : -INFINITY;
-        tm = fmaxf(tm, s[b][i]);
-      }
-    tm = fmaxf(tm, __shfl_xor(tm, 32, 64));
-    const float al = exp2f(mx - tm);
-    mx = tm;
-    l *= al;
-#pragma unroll
-    for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[d][i] *= al;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {  // 16 keys at a time
-      bf16x8_t pf;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const __bf16 p = (__bf16)exp2f(s[g >> 1][(g & 1) * 8 + i] - mx);
-        pf[i] = p;
-        l += (float)p;
-      }
-#pragma unroll
-      for (int d = 0; d < HD / 32; ++d) {
-        bf16x8_t vf;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          vf[i] = __builtin_bit_cast(__bf16, vtile[(g * 16 + (i >> 2) * 8 + hl * 4 + (i & 3)) * KP + d * 32 + (lane & 31)]);
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[d], 0, 0, 0);
-      }
+        for (int i = 0; i < 16; ++i)
+          if (b * kKB + kb * 32 + (i >> 2) * 8 + hl * 4 + (i & 3) >= L) s[kb][i] = -INFINITY;
     }
+    // probabilities against the running max, rounded to bf16 in the order of the scores; the sum is of the rounded ones
+    bf16x8_t pf[4];
+    auto probabilities = [&]() __attribute__((always_inline)) {
+      float t0 = 0.f, t1 = 0.f;
+      const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = (g & 1) * 8 + 2 * e;
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[g >> 1][i], sl2, -mx));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[g >> 1][i + 1], sl2, -mx));
+          const bf16x2_t pk = {(__bf16)p0, (__bf16)p1};
+          if (e & 1) t1 = __builtin_amdgcn_fdot2_f32_bf16(pk, one, t1, false);
+          else t0 = __builtin_amdgcn_fdot2_f32_bf16(pk, one, t0, false);
+          w[e] = __builtin_bit_cast(uint32_t, pk);
+        }
+        pf[g] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
+      }
+      return t0 + t1;
+    };
+    float t = probabilities();
+    if (__any(!(t <= kLazyMax))) {
+      float tm = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) tm = fmaxf(tm, s[kb][i]);
+      tm = fmaxf(mx, fmaxf(tm, __shfl_xor(tm, 32, 64)) * sl2);
+      const float al = __builtin_amdgcn_exp2f(mx - tm);
+      mx = tm;
+      l *= al;
+#pragma unroll
+      for (int db = 0; db < HD / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= al;
+      t = probabilities();
+    }
+    l += t;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int db = 0; db < HD / 32; ++db) {
+        bf16x4_t v[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          v[e] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+              (__attribute__((address_space(3))) bf16x4_t*)(lbase + vf[db] + st * STAGE + (g * 16 + e * 8) * ROWB));
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7), pf[g],
+                                                        o[db], 0, 0, 0);
+      }
+    read_ahead<4 * HD / 32, 2, 2>();
+    // this wave's loads have landed and its reads returned; behind the barrier everyone's have
+    wait_vmcnt0_lgkmcnt0();
+    asm volatile("s_barrier" ::: "memory");
+  };
+  wait_vmcnt0_lgkmcnt0();
+  asm volatile("s_barrier" ::: "memory");
+  using NoMask = std::false_type;
+  using Mask = std::true_type;
+  // only a request's last block, which is the last of its list, can hold keys past L
+  const int whole = cnt > 0 && L % kKB != 0 && block_at(cnt - 1) == nkb - 1 ? cnt - 1 : cnt;
+  int j = 0, b = cnt > 0 ? block_at(0) : 0;
+  auto after = [&](int i) __attribute__((always_inline)) { return i + 1 < cnt ? block_at(i + 1) : -1; };
+  for (; j + 1 < whole; j += 2) {
+    const int b1 = after(j);
+    step(b, b1, S0{}, NoMask{});
+    b = after(j + 1);
+    step(b1, b, S1{}, NoMask{});
+  }
+  if (j < whole) {
+    const int b1 = after(j);
+    step(b, b1, S0{}, NoMask{});
+    b = b1;
+    ++j;
+  }
+  if (j < cnt) {
+    if ((j & 1) == 0) step(b, -1, S0{}, Mask{});
+    else step(b, -1, S1{}, Mask{});
   }
   l += __shfl_xor(l, 32, 64);
   if (qrow < L) {
@@ -405,9 +527,9 @@ hipError_t launch_attention_sparse(int dtype, const void* q, const void* k, cons
   if (dtype == DIT_F32)
     hipLaunchKernelGGL(sparse_f32_kernel, dim3((unsigned)nqb * (kQB / FQ), (unsigned)heads), dim3(256), 0, s, a);
   else if (head_dim == 64)
-    hipLaunchKernelGGL(sparse_bf16_kernel<64>, dim3((unsigned)nqb, (unsigned)heads), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(sparse_bf16_kernel<64>, dim3((unsigned)nqb * heads), dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL(sparse_bf16_kernel<128>, dim3((unsigned)nqb, (unsigned)heads), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(sparse_bf16_kernel<128>, dim3((unsigned)nqb * heads), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
