@@ -28,44 +28,84 @@ __device__ __forceinline__ int request_of(const int* off, int n, int row) {
 }
 
 // ---------------------------------------------------------------- means
-// Block (unit, head): the mean of one block of keys or queries, 64 bits.
-// Threads (token slot, 8 dimensions); the slots' sums meet in LDS.
-template <typename T, int HD>
+// Where the mean of key block u (over all requests) has dimension d (even) of
+// head h: in the order in which the matrix cores take it, 16 blocks at a time, so
+// that the lanes of a wave load neighbouring words.  (From rows, 16 lanes would
+// each start a row of their own: 80 accesses of the vector cache a load, 208 us
+// at 516 x 1032 blocks and 24 heads.)
+__device__ __forceinline__ long key_mean_at(const SparseMeta& m, int hd, int h, int u, int d) {
+  const long tile = (long)h * ((m.kb_off[m.n_req] + 15) >> 4) + (u >> 4);
+  return ((tile * (hd >> 3) + (d >> 3)) * 64 + (d >> 1 & 3) * 16 + (u & 15)) * 2;
+}
+
+// Block (key or query block, 512 columns of [heads, head_dim]): its mean, 64
+// bits.  A wave reads 1 KB of a token's row at a time and takes every fourth
+// token; the waves' sums meet in LDS.  Every element of Q and K is read once.
+template <typename T>
 __global__ __launch_bounds__(256) void block_means_kernel(const T* __restrict__ q, const T* __restrict__ k, int heads,
-                                                          const SparseMeta m, double* __restrict__ qm,
+                                                          int hd, const SparseMeta m, double* __restrict__ qm,
                                                           double* __restrict__ km) {
-  constexpr int CH = HD / 8, SL = 256 / CH;
-  __shared__ double part[SL][HD + 1];
+  __shared__ double part[4][8][65];
   const int nkb = m.kb_off[m.n_req];
   int u = blockIdx.x;
-  const int h = blockIdx.y;
   const bool keys = u < nkb;
   if (!keys) u -= nkb;
   const int* off = keys ? m.kb_off : m.qb_off;
   const int bs = keys ? kKB : kQB;
   const int r = request_of(off, m.n_req, u);
   const int L = m.off[r + 1] - m.off[r], t0 = (u - off[r]) * bs, n = min(bs, L - t0);
-  const int c = threadIdx.x % CH, sl = threadIdx.x / CH;
-  const T* x = (keys ? k : q) + ((long)(m.off[r] + t0) * heads + h) * HD + c * 8;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int width = heads * hd, col = (blockIdx.y * 64 + lane) * 8;
   double a[8] = {};
-  for (int t = sl; t < n; t += SL) {
-    const T* y = x + (long)t * heads * HD;
+  if (col < width) {
+    const T* x = (keys ? k : q) + (long)(m.off[r] + t0) * width + col;
+#pragma unroll 1
+    for (int t = wave; t < n; t += 64) {
+      float v[16][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) a[i] += (double)to_f32<T>(y[i]);
+      for (int i = 0; i < 16; ++i) {
+        const int tt = min(t + 4 * i, n - 1);  // past the end: the last token again, not added
+        if constexpr (sizeof(T) == 2) {
+          const uint4 w = *(const uint4*)(x + (long)tt * width);
+          const uint32_t e[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            v[i][2 * c] = __uint_as_float(e[c] << 16);
+            v[i][2 * c + 1] = __uint_as_float(e[c] & 0xffff0000u);
+          }
+        } else {
+          *(float4*)&v[i][0] = ((const float4*)(x + (long)tt * width))[0];
+          *(float4*)&v[i][4] = ((const float4*)(x + (long)tt * width))[1];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (t + 4 * i < n) {
+#pragma unroll
+          for (int c = 0; c < 8; ++c) a[c] += (double)v[i][c];
+        }
+    }
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) part[sl][c * 8 + i] = a[i];
+  for (int c = 0; c < 8; ++c) part[wave][c][lane] = a[c];
   __syncthreads();
-  if (threadIdx.x < HD) {
-    double s = 0.0;
-    for (int i = 0; i < SL; ++i) s += part[i][threadIdx.x];
-    const long row = (long)h * off[m.n_req] + u;
-    (keys ? km : qm)[row * HD + threadIdx.x] = s / n;
+  // two neighbouring columns per thread
+  const int chunk = threadIdx.x >> 2, c = (threadIdx.x & 3) * 2, e = (blockIdx.y * 64 + chunk) * 8 + c;
+  if (e >= width) return;
+  double2 s = make_double2(0.0, 0.0);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    s.x += part[w][c][chunk];
+    s.y += part[w][c + 1][chunk];
   }
+  const int h = e / hd, d = e - h * hd;
+  const double2 mean = make_double2(s.x / n, s.y / n);
+  if (keys) *(double2*)(km + key_mean_at(m, hd, h, u, d)) = mean;
+  else *(double2*)(qm + ((long)h * m.qb_off[m.n_req] + u) * hd + d) = mean;
 }
 
 // ---------------------------------------------------------------- selection
-// order-preserving bits of a score: larger scores, larger keys; -0 as 0, NaN above all
+// order-preserving bits of a score: larger scores, larger keys; -0 as 0, NaN above all; never 0
 __device__ __forceinline__ uint64_t score_key(double s) {
   if (s != s) return ~0ull - 1;
   s += 0.0;
@@ -73,55 +113,200 @@ __device__ __forceinline__ uint64_t score_key(double s) {
   return b >> 63 ? ~b : b | (1ull << 63);
 }
 
-template <int HD>
-__global__ __launch_bounds__(256) void select_blocks_kernel(const double* __restrict__ qm, const double* __restrict__ km,
-                                                            const SparseMeta m, int text_first, int keep,
-                                                            int* __restrict__ out) {
-  __shared__ double qs[HD];
-  __shared__ uint64_t key[kSparseMaxKeyBlocks];
-  const int row = blockIdx.x, h = blockIdx.y;
-  const int r = request_of(m.qb_off, m.n_req, row);
-  const int n = m.kb_off[r + 1] - m.kb_off[r];
-  const int nt = text_first ? (m.n_txt[r] + kKB - 1) / kKB : 0;
-  const int tid = threadIdx.x;
-  for (int i = tid; i < HD; i += 256) qs[i] = qm[((long)h * m.qb_off[m.n_req] + row) * HD + i];
-  __syncthreads();
-  for (int j = tid; j < n; j += 256) {
-    const double* y = km + ((long)h * m.kb_off[m.n_req] + m.kb_off[r] + j) * HD;
-    double s = 0.0;
-    for (int i = 0; i < HD; ++i) s += qs[i] * y[i];
-    key[j] = j < nt ? ~0ull : score_key(s);
-  }
-  __syncthreads();
-  if (tid >= 64) return;
-  int* o = out + ((long)h * m.qb_off[m.n_req] + row) * keep;
-  const int lane = tid, want = min(keep, n);
-  // t: the want-th largest key, bit by bit; done early when exactly `want` keys reach it
-  uint64_t t = 0;
-  if (want < n) {
-    for (int bit = 63; bit >= 0; --bit) {
-      const uint64_t c = t | 1ull << bit;
-      int count = 0;
-      for (int j = 0; j < n; j += 64) count += __popcll(__ballot(j + lane < n && key[min(j + lane, n - 1)] >= c));
-      if (count >= want) t = c;
-      if (count == want) break;
+struct SelectRows {
+  int off[kMaxReq + 1];  // groups of query blocks of one request
+};
+typedef double f64x4_t __attribute__((ext_vector_type(4)));
+
+// how many of the wave's keys are at least c (c > 0; a key that does not count is 0)
+template <int NV>
+__device__ __forceinline__ int count_from(const uint32_t* key, uint32_t c) {
+  int count = 0;
+#pragma unroll
+  for (int v = 0; v < NV; ++v) count += __popcll(__ballot(key[v] >= c));
+  return count;
+}
+// The largest t that at least `want` keys reach, bit by bit; *exact: exactly so many do (which ends the search early).
+template <int NV>
+__device__ __forceinline__ uint32_t nth_largest(const uint32_t* key, int want, bool* exact) {
+  uint32_t t = 0;
+  *exact = false;
+  for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
+    const int count = count_from<NV>(key, t | bit);
+    if (count >= want) t |= bit;
+    if (count == want) {
+      *exact = true;
+      break;
     }
   }
-  int above = 0;
-  for (int j = 0; j < n; j += 64) above += __popcll(__ballot(j + lane < n && key[min(j + lane, n - 1)] > t));
-  int ties = want - above, at = 0;  // of the keys equal to t, the first `ties` belong to the answer
-  for (int j = 0; j < n; j += 64) {
-    const bool in = j + lane < n;
-    const uint64_t k = key[min(j + lane, n - 1)];
-    const uint64_t below = (1ull << lane) - 1;
-    const uint64_t eq = __ballot(in && k == t);
-    const bool take = in && (k > t || (k == t && __popcll(eq & below) < ties));
-    const uint64_t tk = __ballot(take);
-    if (take) o[at + __popcll(tk & below)] = j + lane;
-    at += __popcll(tk);
-    ties -= min(ties, (int)__popcll(eq));
+  return t;
+}
+// the high word's score, its low word taken as 0
+__device__ __forceinline__ double key_score(uint32_t hi) {
+  const uint32_t b = hi >> 31 ? hi ^ 0x80000000u : ~hi;
+  return __longlong_as_double((long long)((uint64_t)b << 32));
+}
+// A t that exactly `want` keys reach, by halving the interval of the scores: about
+// as many steps as bits tell the want-th score from the next (10 of 1000 normal
+// ones), where the search over the keys' bits also walks through the exponent.  0
+// where it ends without one: equal high words, infinities, NaN.
+template <int NV>
+__device__ __forceinline__ uint32_t halve_scores(const uint32_t* key, int want) {
+  uint32_t lo = ~0u, hi = 0;
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    lo = min(lo, key[v] - 1);  // keys that do not count: the largest
+    hi = max(hi, key[v]);
   }
-  for (int j = want + lane; j < keep; j += 64) o[j] = -1;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    lo = min(lo, (uint32_t)__shfl_xor((int)lo, o, 64));
+    hi = max(hi, (uint32_t)__shfl_xor((int)hi, o, 64));
+  }
+  double a = key_score(lo + 1), b = key_score(hi);
+  for (int i = 0; i < 24; ++i) {
+    const double mid = 0.5 * (a + b);
+    if (!(mid > a && mid < b)) break;
+    const uint32_t c = (uint32_t)(score_key(mid) >> 32);
+    const int count = count_from<NV>(key, c);
+    if (count == want) return c;
+    if (count > want) a = mid;
+    else b = mid;
+  }
+  return 0;
+}
+
+// NW waves, up to R query blocks of one request and head.  Scores by the 64-bit
+// matrix cores (v_mfma_f64_16x16x4_f64: 16 key blocks x 16 query blocks; of every 8
+// dimensions a lane quarter holds two, in the same order on both sides),
+// kept in LDS as order-preserving integers, high and low words apart.  Then a
+// wave takes a query block, 64 NV scores in registers, and finds the keep-th
+// largest: by the high words, and by the low words among equal ones.
+template <int HD, int NV, int R, int NW>
+__global__ __launch_bounds__(NW * 64) void select_blocks_kernel(const double* __restrict__ qm,
+                                                                const double* __restrict__ km, const SparseMeta m,
+                                                                const SelectRows g, int text_first, int keep,
+                                                                int* __restrict__ out) {
+  constexpr int N = NV * 64;
+  __shared__ uint32_t high[R][N], low[R][N];
+  const int groups = g.off[m.n_req];
+  // blocks of one XCD take consecutive units, head by head: its L2 holds their key means
+  const int unit = xcd_remap(blockIdx.x, gridDim.x);
+  const int h = unit / groups, id = unit - h * groups;
+  const int r = request_of(g.off, m.n_req, id);
+  const int row0 = m.qb_off[r] + (id - g.off[r]) * R, rows = min(R, m.qb_off[r + 1] - row0);
+  const int n = m.kb_off[r + 1] - m.kb_off[r];
+  const int nt = text_first ? (m.n_txt[r] + kKB - 1) / kKB : 0;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lr = lane & 15, lq = lane >> 4;
+  {
+    double2 q[HD / 8];
+    const double* qs = qm + ((long)h * m.qb_off[m.n_req] + row0 + min(lr, rows - 1)) * HD + lq * 2;
+#pragma unroll
+    for (int i = 0; i < HD / 8; ++i) q[i] = *(const double2*)(qs + 8 * i);
+    const int k0 = m.kb_off[r];
+    const double* ks = km + key_mean_at(m, HD, h, 0, 0) + lane * 2;
+    for (int t = (k0 >> 4) + wave; t * 16 < k0 + n; t += NW) {
+      const double* y = ks + (long)t * HD * 16;
+      f64x4_t s = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+      for (int i = 0; i < HD / 8; ++i) {
+        const double2 kv = *(const double2*)(y + i * 128);
+        s = __builtin_amdgcn_mfma_f64_16x16x4f64(kv.x, q[i].x, s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f64_16x16x4f64(kv.y, q[i].y, s, 0, 0, 0);
+      }
+      if (lr < rows)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = t * 16 + lq + 4 * e - k0;  // the first and the last tile hold other requests' blocks, too
+          if (key >= 0 && key < n) {
+            const uint64_t b = score_key(s[e]);
+            high[lr][key] = (uint32_t)(b >> 32);
+            low[lr][key] = (uint32_t)b;
+          }
+        }
+    }
+  }
+  __syncthreads();
+  const int want = min(keep, n);
+  for (int row = wave; row < rows; row += NW) {
+    int* o = out + ((long)h * m.qb_off[m.n_req] + row0 + row) * keep;
+    // The text's blocks, then the best of the others: `best` of them.  Keys that take no part are 0.
+    uint32_t hi[NV], lo[NV], t = 1, tl = 0;
+    const int text = min(nt, want), best = want - text;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int key = v * 64 + lane;
+      const bool in = key >= nt && key < n && best > 0;
+      hi[v] = in ? high[row][key] : 0;
+      lo[v] = in ? low[row][key] : 0;
+    }
+    bool exact = true;
+    int ties = 0;  // of the keys equal to (t, tl), as many belong to the answer
+    if (best > 0 && want < n) {
+      t = halve_scores<NV>(hi, best);
+      if (t == 0) t = nth_largest<NV>(hi, best, &exact);
+    }
+    if (!exact) {
+      uint32_t l[NV];
+#pragma unroll
+      for (int v = 0; v < NV; ++v) l[v] = hi[v] == t ? lo[v] : 0;
+      const int above = t == ~0u ? 0 : count_from<NV>(hi, t + 1);
+      bool found;
+      tl = nth_largest<NV>(l, best - above, &found);
+      ties = best - above;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) ties -= __popcll(__ballot(hi[v] == t && lo[v] > tl));
+    }
+    int at = 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const uint64_t below = (1ull << lane) - 1;
+      bool take = hi[v] >= t;
+      if (!exact) {
+        const bool same = hi[v] == t && lo[v] == tl;
+        const uint64_t eq = __ballot(same);
+        take = hi[v] > t || (hi[v] == t && lo[v] > tl) || (same && __popcll(eq & below) < ties);
+        ties -= min(ties, (int)__popcll(eq));
+      }
+      take = take || v * 64 + lane < text;
+      const uint64_t tk = __ballot(take);
+      if (take) o[at + __popcll(tk & below)] = v * 64 + lane;
+      at += __popcll(tk);
+    }
+    for (int j = want + lane; j < keep; j += 64) o[j] = -1;
+  }
+}
+
+template <int HD, int NV, int R, int NW>
+void launch_select(const double* qm, const double* km, int heads, const SparseMeta& m, int text_first, int keep, int* out,
+                   hipStream_t s) {
+  SelectRows g{};
+  for (int r = 0; r < m.n_req; ++r) g.off[r + 1] = g.off[r] + (m.qb_off[r + 1] - m.qb_off[r] + R - 1) / R;
+  hipLaunchKernelGGL((select_blocks_kernel<HD, NV, R, NW>), dim3((unsigned)g.off[m.n_req] * heads), dim3(NW * 64), 0, s,
+                     qm, km, m, g, text_first, keep, out);
+}
+
+// Query blocks per thread block: 16, which fill the matrix cores' columns; 4 where
+// that leaves CUs idle and the scores are few; 8 where 16 rows of scores exceed
+// LDS.
+template <int HD>
+void launch_select(const double* qm, const double* km, int heads, const SparseMeta& m, int text_first, int keep, int* out,
+                   hipStream_t s) {
+  int n = 0;
+  for (int r = 0; r < m.n_req; ++r) n = std::max(n, m.kb_off[r + 1] - m.kb_off[r]);
+  const bool few = (long)m.qb_off[m.n_req] * heads < 512 * 16;
+  if (n <= 128) {
+    if (few) launch_select<HD, 2, 4, 4>(qm, km, heads, m, text_first, keep, out, s);
+    else launch_select<HD, 2, 16, 4>(qm, km, heads, m, text_first, keep, out, s);
+  } else if (n <= 320) {
+    if (few) launch_select<HD, 5, 4, 4>(qm, km, heads, m, text_first, keep, out, s);
+    else launch_select<HD, 5, 16, 4>(qm, km, heads, m, text_first, keep, out, s);
+  } else if (n <= 1088) {
+    launch_select<HD, 17, 16, 16>(qm, km, heads, m, text_first, keep, out, s);
+  } else {
+    launch_select<HD, 32, 8, 16>(qm, km, heads, m, text_first, keep, out, s);
+  }
 }
 
 // ---------------------------------------------------------------- a query block's list
@@ -496,18 +681,15 @@ __global__ __launch_bounds__(256) void sparse_f32_kernel(const SparseArgs a) {
 
 hipError_t launch_attention_select(int dtype, const void* q, const void* k, int heads, int head_dim, const SparseMeta& m,
                                    int text_first, int keep, double* qm, double* km, int* out, hipStream_t s) {
-  const int nqb = m.qb_off[m.n_req], nkb = m.kb_off[m.n_req];
-  const dim3 gm((unsigned)(nqb + nkb), (unsigned)heads), gs((unsigned)nqb, (unsigned)heads);
-#define DIT_MEANS(T, HD)                                                                                            \
-  hipLaunchKernelGGL((block_means_kernel<T, HD>), gm, dim3(256), 0, s, (const T*)q, (const T*)k, heads, m, qm, km)
-  if (dtype == DIT_F32) DIT_MEANS(float, 64);
-  else if (head_dim == 64) DIT_MEANS(bf16_t, 64);
-  else DIT_MEANS(bf16_t, 128);
-#undef DIT_MEANS
-  if (head_dim == 64)
-    hipLaunchKernelGGL(select_blocks_kernel<64>, gs, dim3(256), 0, s, qm, km, m, text_first, keep, out);
+  const dim3 grid((unsigned)(m.qb_off[m.n_req] + m.kb_off[m.n_req]), (unsigned)((heads * head_dim + 511) / 512));
+  if (dtype == DIT_F32)
+    hipLaunchKernelGGL(block_means_kernel<float>, grid, dim3(256), 0, s, (const float*)q, (const float*)k, heads, head_dim, m,
+                       qm, km);
   else
-    hipLaunchKernelGGL(select_blocks_kernel<128>, gs, dim3(256), 0, s, qm, km, m, text_first, keep, out);
+    hipLaunchKernelGGL(block_means_kernel<bf16_t>, grid, dim3(256), 0, s, (const bf16_t*)q, (const bf16_t*)k, heads,
+                       head_dim, m, qm, km);
+  if (head_dim == 64) launch_select<64>(qm, km, heads, m, text_first, keep, out, s);
+  else launch_select<128>(qm, km, heads, m, text_first, keep, out, s);
   return hipGetLastError();
 }
 

@@ -1127,7 +1127,7 @@ dit_status dit_attention_select_workspace_size(const dit_batch* batch, int heads
   SparseMeta m;
   if ((st = check_sparse(batch, heads, head_dim, dtype, &m))) return st;
   if (!bytes) return fail(DIT_ERR_INVALID_ARG, "bytes is NULL");
-  *bytes = means_bytes(m.qb_off[m.n_req], heads, head_dim) + means_bytes(m.kb_off[m.n_req], heads, head_dim);
+  *bytes = means_bytes(m.qb_off[m.n_req], heads, head_dim) + means_bytes((m.kb_off[m.n_req] + 15) / 16 * 16, heads, head_dim);
   return DIT_OK;
 }
 
@@ -1142,9 +1142,11 @@ dit_status dit_attention_select(const dit_batch* batch, int heads, int head_dim,
   if (!q || !k || !blocks) return fail(DIT_ERR_INVALID_ARG, "q / k / blocks is NULL");
   if (!aligned16(q) || !aligned16(k)) return fail(DIT_ERR_INVALID_ARG, "q / k must be 16-byte aligned");
   if (!aligned_to(blocks, 4)) return fail(DIT_ERR_INVALID_ARG, "blocks must be 4-byte aligned");
-  const int nqb = m.qb_off[m.n_req], nkb = m.kb_off[m.n_req];
+  const int nqb = m.qb_off[m.n_req];
   const size_t qb = means_bytes(nqb, heads, head_dim);
-  if ((st = check_ws(ws, ws_bytes, qb + means_bytes(nkb, heads, head_dim)))) return st;
+  size_t need = 0;
+  dit_attention_select_workspace_size(batch, heads, head_dim, dtype, &need);
+  if ((st = check_ws(ws, ws_bytes, need))) return st;
   double f = 0;
   for (int r = 0; r < m.n_req; ++r)
     f += 2.0 * (m.qb_off[r + 1] - m.qb_off[r]) * (m.kb_off[r + 1] - m.kb_off[r]) * heads * head_dim;

@@ -292,7 +292,7 @@ struct SparseMeta {
   int kb_off[kMaxReq + 1];  // key blocks
   int n_txt[kMaxReq];
 };
-// qm, km: scratch for the means, heads * head_dim * (query blocks) and * (key blocks)
+// qm, km: scratch for the means, heads * head_dim * (query blocks) and * (key blocks up to a multiple of 16)
 hipError_t launch_attention_select(int dtype, const void* q, const void* k, int heads, int head_dim, const SparseMeta& m,
                                    int text_first, int keep, double* qm, double* km, int* out, hipStream_t s);
 hipError_t launch_attention_sparse(int dtype, const void* q, const void* k, const void* v, const int* blocks, int keep,

@@ -251,6 +251,33 @@ def test_select_ties_zeros_and_non_finite_scores(dtype, d):
             assert np.array_equal(_select(b, 1, d, dtype, q.cuda(), k.cuda(), keep), _ref_select(q, k, lens, [0], keep))
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_select_text_with_nan_and_equal_scores(dtype, d):
+    """NaN and infinite scores inside and behind the text's blocks, lists no longer than the text, and scores that
+    differ in their last bits only."""
+    b, lens = _batch([(30, 30, 130)])   # 1030 tokens: 17 key blocks, 3 of them text
+    q, k, _ = _qkv(13, 1030, 2, d, dtype)
+    q = q.abs()
+    k[5, 0, 0] = k[64 * 9, 0, 3] = float("nan")
+    k[64 * 4, 1, 0] = float("inf")
+    k[70, 1, 0] = -float("inf")
+    with np.errstate(invalid="ignore"):
+        for keep in (1, 2, 3, 4, 5, 9, 16, 17, 20):
+            for t in (0, 130):
+                got = _select(b, 2, d, dtype, q.cuda(), k.cuda(), keep, dit.DIT_SELECT_TEXT if t else 0)
+                assert np.array_equal(got, _ref_select(q, k, lens, [t], keep)), (keep, t)
+    # scores 1 + j 2^-40: equal high words, told apart by the low ones alone
+    q = q * 0
+    q[:, :, 0], q[:, :, 1] = 1.0, 2.0 ** -20
+    k = k.nan_to_num(0.0, 0.0, 0.0) * 0
+    k[:, :, 0] = 1.0
+    order = np.random.default_rng(3).permutation(17)
+    for j in range(17):
+        k[j * 64:(j + 1) * 64, :, 1] = float(order[j] % 12) * 2.0 ** -20
+    for keep in (1, 5, 11, 16):
+        assert np.array_equal(_select(b, 2, d, dtype, q.cuda(), k.cuda(), keep), _ref_select(q, k, lens, [0], keep)), keep
+
+
 def test_select_and_attend_at_the_largest_request():
     """2048 key blocks, the most a request may hold: the last block chosen and read."""
     torch = _torch()

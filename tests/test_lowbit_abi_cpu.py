@@ -70,8 +70,8 @@ def _batch(*lens):
 def test_block_counts_and_workspaces():
     assert dit.attention_query_blocks(_batch(1)) == 1
     assert dit.attention_query_blocks(_batch(128, 129, 1)) == 4
-    # means of 3 + 1 query blocks and 5 + 1 key blocks in 64 bits, each part rounded up to 256 bytes
-    assert dit.attention_select_workspace_size(_batch(300, 64), 3, 64, BF) == 4 * 3 * 64 * 8 + 6 * 3 * 64 * 8
+    # means of 3 + 1 query blocks and 5 + 1 key blocks (up to 16) in 64 bits
+    assert dit.attention_select_workspace_size(_batch(300, 64), 3, 64, BF) == 4 * 3 * 64 * 8 + 16 * 3 * 64 * 8
     assert dit.attention_sparse_workspace_size(_batch(300, 64), 3, 64, BF) == 0
     most = dit.DIT_SPARSE_MAX_KEY_BLOCKS * dit.DIT_SPARSE_KEYS
     dit.attention_select_workspace_size(_batch(most), 1, 64, BF)
