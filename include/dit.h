@@ -259,7 +259,7 @@ dit_status dit_linear(int M, int N, int K, int dtype, const void* x, const void*
  *  - codes: one byte each, [rows][128 Kb], zeros past column K;
  *  - scales: one byte each, s = 2^(byte - 127), [ceil(rows / block_rows)][Kb
  *    rounded up to a multiple of 4], 127 past the last block of K.
- * dit_fp8_layout returns the bytes of both buffers.  rows >= 0, 1 <= K <= 2^24.
+ * dit_fp8_layout returns the bytes of both buffers.  rows >= 0, 1 <= K <= 2^22.
  */
 #define DIT_FP8_BLOCK 128
 dit_status dit_fp8_layout(int rows, int K, int block_rows, size_t* code_bytes, size_t* scale_bytes);
@@ -289,7 +289,7 @@ dit_status dit_quantize_fp8(int rows, int K, int block_rows, int dtype, const vo
  *    own rounding.
  * An output's bits depend on its row of X, its row of W, M and N, not on other
  * rows' values, and are the same on every call.  Codes 16-byte aligned, scales
- * 4-byte aligned, b and y aligned to their elements.
+ * 4-byte aligned, b and y aligned to their elements; M * N <= 2^36.
  */
 dit_status dit_linear_fp8(int M, int N, int K, const void* x_codes, const void* x_scales, const void* w_codes,
                           const void* w_scales, const void* b, int b_dtype, void* y, int out_dtype, void* stream);

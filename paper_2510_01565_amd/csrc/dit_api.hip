@@ -696,7 +696,8 @@ dit_status noalloc_scratch(hipStream_t stream, void** out) {
   return DIT_OK;
 }
 // ---------------------------------------------------------------------------- 8-bit matrices
-constexpr int kFp8MaxK = 1 << 24;
+constexpr int kFp8MaxK = 1 << 22;             // bytes of a row: offsets within 256 rows fit 32 bits
+constexpr double kFp8MaxOutputs = 1L << 36;   // blocks of the smallest tiles: fewer than 2^23
 
 dit_status check_fp8_shape(int rows, int K, int block_rows) {
   if (rows < 0 || K <= 0) return fail(DIT_ERR_INVALID_ARG, "rows %d K %d", rows, K);
@@ -1096,6 +1097,7 @@ dit_status dit_linear_fp8(int M, int N, int K, const void* x_codes, const void* 
   if ((st = check_fp8_shape(M, K, 1))) return st;
   if (out_dtype != DIT_F32 && out_dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "out_dtype %d", out_dtype);
   if (b_dtype != DIT_F32 && b_dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "b_dtype %d", b_dtype);
+  if ((double)M * N > kFp8MaxOutputs) return fail(DIT_ERR_UNSUPPORTED, "M %d x N %d exceeds 2^36", M, N);
   if (M == 0) return DIT_OK;
   if (!x_codes || !x_scales || !w_codes || !w_scales || !y)
     return fail(DIT_ERR_INVALID_ARG, "x / w codes or scales or y is NULL");

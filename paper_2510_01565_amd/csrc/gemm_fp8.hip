@@ -47,8 +47,7 @@ __device__ __forceinline__ float scale_of(uint32_t byte) {
 }
 
 // one lane's 32 codes as bf16 values, 8 to an operand
-__device__ __forceinline__ void to_bf16(const uint4& lo, const uint4& hi, float scale, bf16x8_t* out) {
-  const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+__device__ __forceinline__ void to_bf16(const i32x8_t& w, float scale, bf16x8_t* out) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -60,88 +59,6 @@ __device__ __forceinline__ void to_bf16(const uint4& lo, const uint4& hi, float 
       out[i][4 * j + 2] = b[0];
       out[i][4 * j + 3] = b[1];
     }
-}
-
-// 64 x 64 outputs per block, 32 x 32 per wave, operands straight from memory.
-// W's rows are the matrix cores' rows, so a lane holds four neighbouring columns
-// of one output row.
-template <bool F32>
-__global__ __launch_bounds__(256) void fp8_tile_kernel(const Fp8Problem p) {
-  const int tiles_n = (p.N + 63) / 64;
-  const int id = block_id();
-  const int tm = id / tiles_n, tn = id - tm * tiles_n;
-  if (tm * 64 >= p.M) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int m0 = tm * 64 + (wave >> 1) * 32, n0 = tn * 64 + (wave & 1) * 32;
-  const long Kp = (long)p.kb * kFp8Block;
-  const uint8_t *xr[2], *wr[2], *xsr[2], *wsr[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int m = min(m0 + i * 16 + (lane & 15), p.M - 1), n = min(n0 + i * 16 + (lane & 15), p.N - 1);
-    xr[i] = p.x + m * Kp + (lane >> 4) * 32;
-    wr[i] = p.w + n * Kp + (lane >> 4) * 32;
-    xsr[i] = p.xs + (long)m * p.pitch;
-    wsr[i] = p.ws + (long)(n >> 7) * p.pitch;
-  }
-  f32x4_t acc[2][2] = {};
-  for (int kb = 0; kb < p.kb; ++kb) {
-    uint4 x[2][2], w[2][2];
-    int xs[2], ws[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        x[i][c] = ((const uint4*)(xr[i] + kb * 128))[c];
-        w[i][c] = ((const uint4*)(wr[i] + kb * 128))[c];
-      }
-      xs[i] = xsr[i][kb];
-      ws[i] = wsr[i][kb];
-    }
-    if constexpr (F32) {
-      bf16x8_t xb[2][4], wb[2][4];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        to_bf16(x[i][0], x[i][1], scale_of(xs[i]), xb[i]);
-        to_bf16(w[i][0], w[i][1], scale_of(ws[i]), wb[i]);
-      }
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][c], xb[i][c], acc[i][j], 0, 0, 0);
-    } else {
-      i32x8_t xv[2], wv[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        xv[i] = i32x8_t{(int)x[i][0].x, (int)x[i][0].y, (int)x[i][0].z, (int)x[i][0].w,
-                        (int)x[i][1].x, (int)x[i][1].y, (int)x[i][1].z, (int)x[i][1].w};
-        wv[i] = i32x8_t{(int)w[i][0].x, (int)w[i][0].y, (int)w[i][0].z, (int)w[i][0].w,
-                        (int)w[i][1].x, (int)w[i][1].y, (int)w[i][1].z, (int)w[i][1].w};
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv[j], xv[i], acc[i][j], 0, 0, 0, ws[j], 0, xs[i]);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int m = m0 + i * 16 + (lane & 15);
-    if (m >= p.M) continue;
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int n = n0 + j * 16 + (lane >> 4) * 4 + r;
-        if (n >= p.N) continue;
-        const float v = acc[i][j][r] + bias_at(p, n);
-        if constexpr (F32) ((float*)p.y)[(long)m * p.N + n] = v;
-        else ((bf16_t*)p.y)[(long)m * p.N + n] = f2bf(v);
-      }
-  }
 }
 
 // ---------------------------------------------------------------- 256 x 256 tiles, bf16 output
@@ -179,9 +96,33 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 struct __attribute__((packed, aligned(2))) Bf16x8 {
   u32x4_t v;
 };
+struct __attribute__((packed, aligned(4))) F32x4 {
+  f32x4_t v;
+};
 __device__ __forceinline__ u32x4_t pack8(const float* v) {
   return u32x4_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
 }
+// C neighbouring columns (a multiple of 8) of an output row that ends `left` columns further, at any element's address
+template <bool F32, int C>
+__device__ __forceinline__ void store_columns(char* y, const float* v, int left) {
+  if (left >= C) {
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < C; i += 4) ((F32x4*)(y + i * 4))->v = f32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < C; i += 8) ((Bf16x8*)(y + i * 2))->v = pack8(v + i);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < C - 1; ++i)
+      if (i < left) {
+        if constexpr (F32) ((float*)y)[i] = v[i];
+        else ((bf16_t*)y)[i] = f2bf(v[i]);
+      }
+  }
+}
+
 constexpr int kMaxBlocks256 = 256;  // of fp8_256_kernel: one per CU
 constexpr int kMinKTiles256 = 3;    // its loads run up to three K tiles ahead, into the next output tile at most
 
@@ -361,16 +302,7 @@ __global__ __launch_bounds__(512) void fp8_256_kernel(const Fp8Problem p) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) v[j * 4 + r] = acc[c * 2 + i][j][r] + b[j * 4 + r];
       char* const y = (char*)p.y + ((long)m0 * p.N + n0) * 2 + (long)(c * 32 + i * 16) * pitch + yo;
-      if (mr < p.M - m0 - (c * 32 + i * 16)) {
-        if (n >= 16) {
-          ((Bf16x8*)y)->v = pack8(v);
-          ((Bf16x8*)(y + 16))->v = pack8(v + 8);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 15; ++e)
-            if (e < n) ((bf16_t*)y)[e] = f2bf(v[e]);
-        }
-      }
+      if (mr < p.M - m0 - (c * 32 + i * 16)) store_columns<false, 16>(y, v, n);
     }
   };
 
@@ -490,20 +422,269 @@ __global__ __launch_bounds__(512) void fp8_256_kernel(const Fp8Problem p) {
   static_for<Q>([&](auto cc) { store(cc, prev_m0, prev_n0, bias_stage ^ 1); });
 }
 
+// ---------------------------------------------------------------- smaller tiles, and fp32 output
+// acc += the products of one K tile's fragments.  bf16 output: the 8-bit cores,
+// scales in the instruction; fp32: codes and scales to bf16, four steps of 32.
+template <bool F32, int FM, int FN>
+__device__ __forceinline__ void multiply(const i32x8_t* x, const i32x8_t* w, const int* sx, const int* sw, f32x4_t (*acc)[FN]) {
+  if constexpr (F32) {
+    bf16x8_t xb[FM][4];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) to_bf16(x[i], scale_of(sx[i] & 255), xb[i]);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      bf16x8_t wb[4];
+      to_bf16(w[j], scale_of(sw[j] & 255), wb);
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < FM; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[c], xb[i][c], acc[i][j], 0, 0, 0);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j], x[i], acc[i][j], 0, 0, 0, sw[j], 0, sx[i]);
+  }
+}
+
+// a launch's blocks along x (fewer than 2^32 threads), the rest goes on along y
+constexpr int kRingRowLog2 = 22;
+
+// BM x BN outputs per block; KG groups of WM x WN waves share out the K tiles.  A
+// step is KG K tiles, which arrive by direct-to-LDS loads in a ring of ST stages;
+// the groups' sums meet in LDS at the end, in their order.  As in the kernel
+// above a lane holds 4 FN neighbouring columns of each of its rows.
+template <bool F32, int BM, int BN, int WM, int WN, int KG, int ST>
+__global__ __launch_bounds__(WM* WN* KG * 64) void fp8_ring_kernel(const Fp8Problem p) {
+  constexpr int NW = WM * WN * KG, FM = BM / WM / 16, FN = BN / WN / 16;
+  constexpr int ROWB = 128, UNITS = KG * (BM + BN) / 8, LPW = UNITS / NW;  // loads of 8 rows; per wave and step
+  constexpr int TILE = (BM + BN) * ROWB, SCALES = KG * TILE, STAGE = SCALES + BM * 4 + 256;
+  static_assert(LPW * NW == UNITS && BM % 64 == 0 && BM / 64 < NW && KG <= 4 && 4 % KG == 0, "tile config");
+  static_assert(ST * STAGE <= 160 * 1024 && (KG - 1) * WM * WN * FM * FN * 1024 <= ST * STAGE, "LDS");
+  __shared__ uint4 lds[ST * STAGE / 16];
+  char* const lbase = (char*)lds;
+  const int tn = (p.N + BN - 1) / BN, tm = (p.M + BM - 1) / BM;
+  const int id = (int)(blockIdx.y << kRingRowLog2) + xcd_remap(blockIdx.x, gridDim.x);
+  if (id >= tm * tn) return;
+  int im, in;
+  tile_of(id, tm, tn, im, in);
+  const int m0 = im * BM, n0 = in * BN, KT = p.kb, Kp = KT * kFp8Block, steps = (KT + KG - 1) / KG;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wv / (WM * WN), wm = wv / WN % WM, wn = wv % WN;
+  auto swz = [](int row, int c) { return c ^ ((row >> 1) & 7); };
+
+  // this wave's loads of a step: 8 rows each of X or W of one K tile
+  uint32_t go[LPW];
+#pragma unroll
+  for (int i = 0; i < LPW; ++i) {
+    const int row = (wv * LPW + i) * 8 % (BM + BN) + (lane >> 3);
+    int g = row;
+    if (row >= BM) {  // W's rows dealt out to the fragments
+      constexpr int C = BN / WN;
+      const int w = row - BM, in_wave = w % C, f = in_wave & 15;
+      g = w - in_wave + (f >> 2) * (4 * FN) + (in_wave >> 4) * 4 + (f & 3);
+    }
+    go[i] = (uint32_t)g * (uint32_t)Kp + swz(row, lane & 7) * 16;
+  }
+  auto buffer = [&](const uint8_t* base, int r0, int most, int rows, int pitch) __attribute__((always_inline)) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (long)r0 * pitch), (short)0,
+                                             __builtin_amdgcn_readfirstlane(max(min(rows - r0, most), 0) * pitch), kBufferWord3);
+  };
+  const int sgo = (wv < BM / 64 ? wv * 64 + lane : lane & 1) * p.pitch;
+  auto load = [&](int step, int stage) __attribute__((always_inline)) {
+    char* const at = lbase + stage * STAGE;
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+      const int unit = wv * LPW + i, q = unit * 8 / (BM + BN), row = unit * 8 % (BM + BN), kt = step * KG + q;
+      const bool x = row < BM;
+      // locals, not expressions: the host pass drops the kernel's launch stub otherwise
+      const int vo = (int)go[i], so = kt * ROWB;
+      const __amdgpu_buffer_rsrc_t rs =
+          buffer(x ? p.x : p.w, x ? m0 : n0, kt < KT ? (x ? BM : BN) : 0, x ? p.M : p.N, Kp);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rs, (__attribute__((address_space(3))) void*)(at + q * TILE + row * ROWB), 16, vo, so, 0, 0);
+    }
+    // the scale words of the step's K tiles: X's by the first waves, a row per lane, W's two row blocks' by the others
+    const bool x = wv < BM / 64;
+    const int vo = sgo, so = min(step * KG, KT - 1) & ~3;
+    const __amdgpu_buffer_rsrc_t rs =
+        buffer(x ? p.xs : p.ws, x ? m0 : n0 >> 7, x ? BM : 2, x ? p.M : (p.N + 127) >> 7, p.pitch);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rs, (__attribute__((address_space(3))) void*)(at + SCALES + (x ? wv * 256 : BM * 4)), 4, vo, so, 0, 0);
+  };
+  auto lds16 = [&](int at) __attribute__((always_inline)) {
+    return __builtin_bit_cast(i32x4_t, *(const uint4*)(lbase + at));
+  };
+  auto lds4 = [&](int at) __attribute__((always_inline)) { return __builtin_bit_cast(int, *(const Word*)(lbase + at)); };
+  const int xr = wm * FM * 16 + (lane & 15), wr = BM + wn * FN * 16 + (lane & 15);
+  int xa[2], wa[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    xa[h] = kg * TILE + xr * ROWB + swz(xr, (lane >> 4) + 4 * h) * 16;
+    wa[h] = kg * TILE + wr * ROWB + swz(wr, (lane >> 4) + 4 * h) * 16;
+  }
+  const int sxa = SCALES + xr * 4, swa = SCALES + BM * 4 + (((n0 & 127) + wn * FN * 16) >> 7) * 4;
+  f32x4_t acc[FM][FN] = {};
+  static_for<ST - 1>([&](auto sc) { load(decltype(sc)::value, decltype(sc)::value); });
+  int stage = 0;
+  for (int s = 0; s < steps; ++s) {
+    // step s has landed, this wave's part and, behind the barrier, everyone's; the stage before it is read no more
+    wait_vmcnt<(ST - 2) * (LPW + 1)>();
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    block_barrier();
+    load(s + ST - 1, stage == 0 ? ST - 1 : stage - 1);
+    const int at = stage * STAGE, byte = ((s * KG + kg) & 3) * 8;
+    i32x8_t x[FM], w[FN];
+    int sx[FM], sw[FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      x[i] = __builtin_shufflevector(lds16(at + xa[0] + i * 16 * ROWB), lds16(at + xa[1] + i * 16 * ROWB), 0, 1, 2, 3, 4, 5, 6, 7);
+      sx[i] = lds4(at + sxa + i * 64) >> byte;
+    }
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+      w[j] = __builtin_shufflevector(lds16(at + wa[0] + j * 16 * ROWB), lds16(at + wa[1] + j * 16 * ROWB), 0, 1, 2, 3, 4, 5, 6, 7);
+    const int ws = lds4(at + swa) >> byte;  // a wave's columns lie in one row block of scales
+#pragma unroll
+    for (int j = 0; j < FN; ++j) sw[j] = ws;
+    multiply<F32, FM, FN>(x, w, sx, sw, acc);
+    stage = stage + 1 == ST ? 0 : stage + 1;
+  }
+  wait_vmcnt<0>();
+  __syncthreads();
+  if constexpr (KG > 1) {
+    // sums of groups 1 .. at [group - 1][wave of the group][fragment][lane]
+    uint4* const part = lds + (wv % (WM * WN)) * (FM * FN * 64) + lane;
+    if (kg > 0) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          part[(kg - 1) * WM * WN * FM * FN * 64 + (i * FN + j) * 64] = __builtin_bit_cast(uint4, acc[i][j]);
+    }
+    __syncthreads();
+    if (kg > 0) return;
+#pragma unroll
+    for (int g = 0; g < KG - 1; ++g)
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          acc[i][j] += __builtin_bit_cast(f32x4_t, part[g * WM * WN * FM * FN * 64 + (i * FN + j) * 64]);
+  }
+  const int n = n0 + wn * FN * 16 + (lane >> 4) * (4 * FN);
+  if (n >= p.N) return;
+  float b[4 * FN];
+#pragma unroll
+  for (int i = 0; i < 4 * FN; ++i) b[i] = n + i < p.N ? bias_at(p, n + i) : 0.f;
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const long m = m0 + wm * FM * 16 + i * 16 + (lane & 15);
+    if (m >= p.M) continue;
+    float v[4 * FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[j * 4 + r] = acc[i][j][r] + b[j * 4 + r];
+    store_columns<F32, 4 * FN>((char*)p.y + (m * p.N + n) * (F32 ? 4 : 2), v, p.N - n);
+  }
+}
+
+// ---------------------------------------------------------------- few rows
+__device__ __forceinline__ i32x8_t load32(const uint8_t* p) {
+  return __builtin_shufflevector(((const i32x4_t*)p)[0], ((const i32x4_t*)p)[1], 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// Up to 16 MF rows of X against 16 columns per block: W is read once, straight
+// from memory to registers, and the block's waves share out the K tiles, four in
+// flight each.  Their sums meet in LDS in wave order.
+template <bool F32, int MF, int NW>
+__global__ __launch_bounds__(NW * 64) void fp8_rows_kernel(const Fp8Problem p) {
+  __shared__ f32x4_t part[NW][MF][64];
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 15, n0 = block_id() * 16, Kp = p.kb * kFp8Block;
+  if (block_id() >= (p.N + 15) / 16) return;
+  const uint8_t* const w = p.w + (long)min(n0 + lr, p.N - 1) * Kp + (lane >> 4) * 32;
+  const uint8_t* const ws = p.ws + (long)(n0 >> 7) * p.pitch;
+  const uint8_t *x[MF], *xs[MF];
+#pragma unroll
+  for (int i = 0; i < MF; ++i) {
+    const int m = min(i * 16 + lr, p.M - 1);
+    x[i] = p.x + (long)m * Kp + (lane >> 4) * 32;
+    xs[i] = p.xs + (long)m * p.pitch;
+  }
+  f32x4_t acc[MF][1] = {};
+  constexpr int U = 4;
+  for (int k0 = wv; k0 < p.kb; k0 += NW * U) {
+    i32x8_t wf[U], xf[U][MF];
+    int sw[U], sx[U][MF];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int kt = min(k0 + u * NW, p.kb - 1);  // past the end: loaded again, not multiplied
+      wf[u] = load32(w + (long)kt * 128);
+      sw[u] = ws[kt];
+#pragma unroll
+      for (int i = 0; i < MF; ++i) {
+        xf[u][i] = load32(x[i] + (long)kt * 128);
+        sx[u][i] = xs[i][kt];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k0 + u * NW < p.kb) multiply<F32, MF, 1>(xf[u], &wf[u], sx[u], &sw[u], acc);
+  }
+#pragma unroll
+  for (int i = 0; i < MF; ++i) part[wv][i][lane] = acc[i][0];
+  __syncthreads();
+  if (wv >= MF) return;  // wave i finishes rows 16 i ..
+  f32x4_t s = part[0][wv][lane];
+#pragma unroll
+  for (int g = 1; g < NW; ++g) s += part[g][wv][lane];
+  const int m = wv * 16 + lr, n = n0 + (lane >> 4) * 4;
+  if (m >= p.M) return;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    if (n + r >= p.N) break;
+    const float v = s[r] + bias_at(p, n + r);
+    const long o = (long)m * p.N + n + r;
+    if constexpr (F32) ((float*)p.y)[o] = v;
+    else ((bf16_t*)p.y)[o] = f2bf(v);
+  }
+}
+
 }  // namespace
 
 // Which kernel a product takes.
-enum Fp8Cfg { FP8_TILE, FP8_256 };
+enum Fp8Cfg { FP8_ROWS, FP8_64, FP8_128, FP8_256 };
 static Fp8Cfg pick(int M, int N, int K, int out_dtype) {
-  const long big = (long)((M + 255) / 256) * ((N + 255) / 256);
-  // offsets within a tile of 256 rows fit 32 bits up to 2^22 bytes a row
-  if (out_dtype == DIT_BF16 && fp8_k_blocks(K) >= kMinKTiles256 && K <= 1 << 22 && N <= 1 << 21 && big >= 64) return FP8_256;
-  return FP8_TILE;
+  const long big = (long)((M + 255) / 256) * ((N + 255) / 256), mid = (long)((M + 127) / 128) * ((N + 127) / 128);
+  if (M <= 32) return FP8_ROWS;
+  // offsets within a tile of 256 output rows fit 32 bits up to 2^21 columns
+  if (out_dtype == DIT_BF16 && fp8_k_blocks(K) >= kMinKTiles256 && N <= 1 << 21 && big >= 64) return FP8_256;
+  return mid >= 192 ? FP8_128 : FP8_64;
 }
 
 const char* gemm_fp8_config_name(int M, int N, int K, int out_dtype) {
-  static const char* names[] = {"gemm_fp8_64x64", "gemm_fp8_256x256"};
+  static const char* names[] = {"gemm_fp8_rows", "gemm_fp8_64x64", "gemm_fp8_128x128", "gemm_fp8_256x256"};
   return names[pick(M, N, K, out_dtype)];
+}
+
+template <bool F32, int BM, int BN, int KG, int ST>
+static void launch_ring(const Fp8Problem& p, hipStream_t s) {
+  const long tiles = (long)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN);
+  const dim3 grid((unsigned)std::min(tiles, 1L << kRingRowLog2), (unsigned)((tiles - 1) >> kRingRowLog2) + 1);
+  hipLaunchKernelGGL((fp8_ring_kernel<F32, BM, BN, 2, 2, KG, ST>), grid, dim3(4 * KG * 64), 0, s, p);
+}
+
+template <bool F32>
+static void launch_small(Fp8Cfg cfg, const Fp8Problem& p, hipStream_t s) {
+  const dim3 strips = grid_of(((long)p.N + 15) / 16);
+  if (cfg == FP8_64) launch_ring<F32, 64, 64, 2, 4>(p, s);
+  else if (cfg == FP8_128) launch_ring<F32, 128, 128, 2, 2>(p, s);
+  else if (p.M <= 16) hipLaunchKernelGGL((fp8_rows_kernel<F32, 1, 4>), strips, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((fp8_rows_kernel<F32, 2, 4>), strips, dim3(256), 0, s, p);
 }
 
 hipError_t launch_gemm_fp8(int M, int N, int K, const void* x, const void* xs, const void* w, const void* ws,
@@ -523,15 +704,13 @@ hipError_t launch_gemm_fp8(int M, int N, int K, const void* x, const void* xs, c
   p.pitch = fp8_scale_pitch(K);
   const Fp8Cfg cfg = pick(M, N, K, out_dtype);
   if (cfg == FP8_256) {
-    const long big = (long)((M + 255) / 256) * ((N + 255) / 256);
-    hipLaunchKernelGGL(fp8_256_kernel, dim3((unsigned)std::min<long>(big, kMaxBlocks256)), dim3(512), 0, s, p);
-    return hipGetLastError();
+    const long tiles = (long)((M + 255) / 256) * ((N + 255) / 256);
+    hipLaunchKernelGGL(fp8_256_kernel, dim3((unsigned)std::min<long>(tiles, kMaxBlocks256)), dim3(512), 0, s, p);
+  } else if (out_dtype == DIT_F32) {
+    launch_small<true>(cfg, p, s);
+  } else {
+    launch_small<false>(cfg, p, s);
   }
-  const long tiles = (long)((M + 63) / 64) * ((N + 63) / 64);
-  if (out_dtype == DIT_F32)
-    hipLaunchKernelGGL((fp8_tile_kernel<true>), grid_of(tiles), dim3(256), 0, s, p);
-  else
-    hipLaunchKernelGGL((fp8_tile_kernel<false>), grid_of(tiles), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
