@@ -13,6 +13,8 @@
 // output's own rounding.
 // fp32 output: the codes go through bf16 (exactly, scales included) to the bf16
 // matrix cores, exact products with fp32 sums, at half the rate.
+#include <math.h>
+
 #include "device_common.h"
 
 namespace dit {
@@ -598,14 +600,15 @@ __device__ __forceinline__ i32x8_t load32(const uint8_t* p) {
 }
 
 // Up to 16 MF rows of X against 16 columns per block: W is read once, straight
-// from memory to registers, and the block's waves share out the K tiles, four in
+// from memory to registers, and the block's waves share out the K tiles, two in
 // flight each.  Their sums meet in LDS in wave order.
 template <bool F32, int MF, int NW>
 __global__ __launch_bounds__(NW * 64) void fp8_rows_kernel(const Fp8Problem p) {
   __shared__ f32x4_t part[NW][MF][64];
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lr = lane & 15, n0 = block_id() * 16, Kp = p.kb * kFp8Block;
-  if (block_id() >= (p.N + 15) / 16) return;
+  const int strip = (int)(blockIdx.y << kRingRowLog2) + (int)blockIdx.x;
+  if (strip >= ((uint32_t)p.N + 15) / 16) return;
+  const int lr = lane & 15, n0 = strip * 16, Kp = p.kb * kFp8Block;
   const uint8_t* const w = p.w + (long)min(n0 + lr, p.N - 1) * Kp + (lane >> 4) * 32;
   const uint8_t* const ws = p.ws + (long)(n0 >> 7) * p.pitch;
   const uint8_t *x[MF], *xs[MF];
@@ -616,7 +619,7 @@ __global__ __launch_bounds__(NW * 64) void fp8_rows_kernel(const Fp8Problem p) {
     xs[i] = p.xs + (long)m * p.pitch;
   }
   f32x4_t acc[MF][1] = {};
-  constexpr int U = 4;
+  constexpr int U = 2;
   for (int k0 = wv; k0 < p.kb; k0 += NW * U) {
     i32x8_t wf[U], xf[U][MF];
     int sw[U], sx[U][MF];
@@ -656,14 +659,35 @@ __global__ __launch_bounds__(NW * 64) void fp8_rows_kernel(const Fp8Problem p) {
 
 }  // namespace
 
-// Which kernel a product takes.
+// Which kernel a product takes: the one whose modelled time is least.  In
+// microseconds, rounds of 256 tiles times (a fixed part + a part per K tile of
+// 128), fitted to 25 shapes (M 1 - 8629, N 1536 - 16384, K 256 - 16384; it picks
+// the fastest of the four or one within 8% of it on all of them):
+//   64 x 64      589 x 1536 x 6144 15.2 (128 x 128: 28.9), 589 x 1536 x 1536 6.6
+//   128 x 128    4429 x 1536 x 1536 20.3 (64: 34.3, 256: 25.7), 589 x 6144 x 1536 12.1
+//   256 x 256    4429 x 6144 x 1536 47 (128: 65); a launch of one round leaves the
+//                chip its clock, hence two lines
+//   rows         16 x 1536 x 6144 8.5 (64: 12.7), but 16 x 16384 x 4096 21.7 (64: 12.9),
+//                where X's share of the traffic counts
 enum Fp8Cfg { FP8_ROWS, FP8_64, FP8_128, FP8_256 };
 static Fp8Cfg pick(int M, int N, int K, int out_dtype) {
-  const long big = (long)((M + 255) / 256) * ((N + 255) / 256), mid = (long)((M + 127) / 128) * ((N + 127) / 128);
-  if (M <= 32) return FP8_ROWS;
+  const double kt = fp8_k_blocks(K);
+  const bool f32 = out_dtype == DIT_F32;
+  auto rounds = [&](int t) { return ceil(ceil((double)M / t) * ceil((double)N / t) / 256.0); };
+  Fp8Cfg cfg = FP8_64;
+  double best = 2.0 + rounds(64) * (1.5 + (f32 ? 0.36 : 0.235) * kt);
+  auto offer = [&](Fp8Cfg c, double us) {
+    if (us < best) {
+      best = us;
+      cfg = c;
+    }
+  };
+  offer(FP8_128, 2.0 + rounds(128) * (2.75 + (f32 ? 1.07 : 0.547) * kt));
   // offsets within a tile of 256 output rows fit 32 bits up to 2^21 columns
-  if (out_dtype == DIT_BF16 && fp8_k_blocks(K) >= kMinKTiles256 && N <= 1 << 21 && big >= 64) return FP8_256;
-  return mid >= 192 ? FP8_128 : FP8_64;
+  if (!f32 && kt >= kMinKTiles256 && N <= 1 << 21)
+    offer(FP8_256, rounds(256) <= 1 ? 13.5 + 1.02 * kt : rounds(256) * (7.0 + 1.45 * kt));
+  if (M <= 32) offer(FP8_ROWS, 3.5 + fmax(ceil(N / 16.0) * kt * 2048 * (1 + M / 16.0) / 7e6, kt * (0.045 + 0.004 * M)));
+  return cfg;
 }
 
 const char* gemm_fp8_config_name(int M, int N, int K, int out_dtype) {
@@ -671,20 +695,24 @@ const char* gemm_fp8_config_name(int M, int N, int K, int out_dtype) {
   return names[pick(M, N, K, out_dtype)];
 }
 
-template <bool F32, int BM, int BN, int KG, int ST>
+static dim3 ring_grid(long blocks) {
+  return dim3((unsigned)std::min(blocks, 1L << kRingRowLog2), (unsigned)((blocks - 1) >> kRingRowLog2) + 1);
+}
+
+template <bool F32, int BM, int BN, int WM, int WN, int KG, int ST>
 static void launch_ring(const Fp8Problem& p, hipStream_t s) {
   const long tiles = (long)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN);
-  const dim3 grid((unsigned)std::min(tiles, 1L << kRingRowLog2), (unsigned)((tiles - 1) >> kRingRowLog2) + 1);
-  hipLaunchKernelGGL((fp8_ring_kernel<F32, BM, BN, 2, 2, KG, ST>), grid, dim3(4 * KG * 64), 0, s, p);
+  const dim3 grid = ring_grid(tiles);
+  hipLaunchKernelGGL((fp8_ring_kernel<F32, BM, BN, WM, WN, KG, ST>), grid, dim3(WM * WN * KG * 64), 0, s, p);
 }
 
 template <bool F32>
 static void launch_small(Fp8Cfg cfg, const Fp8Problem& p, hipStream_t s) {
-  const dim3 strips = grid_of(((long)p.N + 15) / 16);
-  if (cfg == FP8_64) launch_ring<F32, 64, 64, 2, 4>(p, s);
-  else if (cfg == FP8_128) launch_ring<F32, 128, 128, 2, 2>(p, s);
-  else if (p.M <= 16) hipLaunchKernelGGL((fp8_rows_kernel<F32, 1, 4>), strips, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((fp8_rows_kernel<F32, 2, 4>), strips, dim3(256), 0, s, p);
+  const dim3 strips = ring_grid(((long)p.N + 15) / 16);
+  if (cfg == FP8_64) launch_ring<F32, 64, 64, 2, 2, 2, 4>(p, s);
+  else if (cfg == FP8_128) launch_ring<F32, 128, 128, 2, 4, 1, 4>(p, s);
+  else if (p.M <= 16) hipLaunchKernelGGL((fp8_rows_kernel<F32, 1, 8>), strips, dim3(512), 0, s, p);
+  else hipLaunchKernelGGL((fp8_rows_kernel<F32, 2, 8>), strips, dim3(512), 0, s, p);
 }
 
 hipError_t launch_gemm_fp8(int M, int N, int K, const void* x, const void* xs, const void* w, const void* ws,

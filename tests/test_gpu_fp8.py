@@ -244,9 +244,23 @@ def _check_large(got, ref, mag, K, out):
     (4097, 4105, 700, "bf16", 1),     # 6, y on an odd element
     (4100, 8200, 900, "f32", 3),      # 8, two to three tiles a block
     (5000, 6001, 1100, "bf16", 0),    # 9
-    (2048, 2049, 1300, None, 5),      # 8 x 9 tiles, one a block
+    (2900, 7100, 1300, None, 5),      # 12 x 28 tiles: some blocks one, some two
 ])
 def test_linear_fp8_256x256(M, N, K, bias, off):
     got, ref, mag, ran = _large(M, N, K, "bf16", bias, K, off)
     assert "gemm_fp8_256x256" in ran, ran
     _check_large(got, ref, mag, K, "bf16")
+
+
+@pytest.mark.parametrize("M,N,K,out,cfg", [
+    (1, 4100, 513, "f32", "rows"), (16, 1000, 6000, "bf16", "rows"), (31, 77, 1300, "f32", "rows"), (32, 48, 128, "bf16", "rows"),
+    (33, 4001, 300, "bf16", "64x64"), (589, 1536, 6144, "f32", "64x64"), (300, 999, 2000, "bf16", "64x64"), (20, 20000, 700, "bf16", "64x64"),
+    (4429, 1530, 1536, "bf16", "128x128"), (4429, 1530, 900, "f32", "128x128"), (4000, 3999, 100, "bf16", "128x128"),
+    (4000, 4001, 257, "f32", "128x128"), (4429, 6144, 1500, "bf16", "256x256"),
+])
+def test_linear_fp8_every_kernel(M, N, K, out, cfg):
+    """Shapes for which the launch model picks each kernel, on misaligned outputs too (off 1); the profile names it."""
+    for off in (0, 1):
+        got, ref, mag, ran = _large(M, N, K, out, "bf16" if off else "f32", M + N + K + off, off)
+        assert "gemm_fp8_" + cfg in ran, ran
+        _check_large(got, ref, mag, K, out)
