@@ -311,9 +311,31 @@ void launch_select(const double* qm, const double* km, int heads, const SparseMe
 
 // ---------------------------------------------------------------- a query block's list
 // The blocks that `keep` entries name, ascending and each once, in `list`;
-// returns how many.  Entries outside [0, n) name none.  mask: kSparseMaxKeyBlocks bits.
-__device__ __forceinline__ int read_list(const int* __restrict__ entries, int keep, int n, uint32_t* mask, uint16_t* list,
-                                         int* count, int tid, int nt) {
+// returns how many.  Entries outside [0, n) name none.  Entries that ascend
+// already, with none out of range but at the end, as the selection writes them,
+// are taken as they stand (one barrier); others pass through a bit mask.
+// scratch: a word for the count, one for each of up to 4 waves, kSparseMaxKeyBlocks bits.
+__device__ __forceinline__ int read_list(const int* __restrict__ entries, int keep, int n, uint32_t* scratch, uint16_t* list,
+                                         int tid, int nt) {
+  uint32_t *const count = scratch, *const plain = scratch + 1, *const mask = scratch + 5;
+  auto in_range = [&](int i) { return i < keep && (uint32_t)entries[min(i, keep - 1)] < (uint32_t)n; };
+  bool ok = true;
+  for (int i = tid; i < keep; i += nt) {
+    const bool in = in_range(i);
+    const int b = entries[i];
+    if (in) {
+      ok = ok && (i == 0 || (in_range(i - 1) && entries[i - 1] < b));
+      list[i] = (uint16_t)b;
+      if (!in_range(i + 1)) *count = i + 1;  // one thread of an ascending list
+    } else if (i == 0) {
+      *count = 0;
+    }
+  }
+  const uint64_t all = __ballot(ok);
+  if ((tid & 63) == 0) plain[tid >> 6] = all == __ballot(true);
+  __syncthreads();
+  if (plain[0] & plain[1] & plain[2] & plain[3]) return *count;
+  __syncthreads();
   for (int i = tid; i < kSparseMaxKeyBlocks / 32; i += nt) mask[i] = 0;
   __syncthreads();
   for (int i = tid; i < keep; i += nt) {
@@ -336,6 +358,7 @@ __device__ __forceinline__ int read_list(const int* __restrict__ entries, int ke
   __syncthreads();
   return *count;
 }
+constexpr int kListScratch = (5 + kSparseMaxKeyBlocks / 32) * 4;  // bytes
 
 struct SparseArgs {
   const void *q, *k, *v;
@@ -383,8 +406,8 @@ void sparse_bf16_kernel(const SparseArgs a) {
   constexpr int ROWB = HD * 2, TILE = kKB * ROWB, STAGE = 2 * TILE;
   // [stage][K tile | V tile], then the list.  One array: with several the compiler waits for all loads ahead of every
   // read of LDS.
-  constexpr int LIST = 2 * STAGE, MASK = LIST + kSparseMaxKeyBlocks * 2, COUNT = MASK + kSparseMaxKeyBlocks / 8;
-  __shared__ uint4 smem[COUNT / 16 + 1];
+  constexpr int LIST = 2 * STAGE, SCRATCH = LIST + kSparseMaxKeyBlocks * 2;
+  __shared__ uint4 smem[(SCRATCH + kListScratch + 15) / 16];
   char* const lbase = (char*)smem;
   uint16_t* const list = (uint16_t*)(lbase + LIST);
   const SparseMeta& m = a.meta;
@@ -400,18 +423,6 @@ void sparse_bf16_kernel(const SparseArgs a) {
   const bf16_t* Q = (const bf16_t*)a.q + base;
   const bf16_t* K = (const bf16_t*)a.k + base;
   const bf16_t* V = (const bf16_t*)a.v + base;
-
-  const int qrow = q0 + wave * 32 + (lane & 31);
-  bf16x8_t qf[HD / 16];
-#pragma unroll
-  for (int s = 0; s < HD / 16; ++s) {
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (qrow < L) u = *(const uint4*)(Q + qrow * tok + (s * 2 + hl) * 8);
-    qf[s] = __builtin_bit_cast(bf16x8_t, u);
-  }
-  const int cnt = __builtin_amdgcn_readfirstlane(
-      read_list(a.blocks + ((long)h * nqb + row) * a.keep, a.keep, nkb, (uint32_t*)(lbase + MASK), list, (int*)(lbase + COUNT),
-                tid, 256));
 
   // slot of chunk c of K row `key`: the 16 rows of a fragment read lie in 16 different 16-byte bank groups
   auto kswz = [](int key, int c) { return HD == 128 ? c ^ (key & 15) : c ^ ((key >> 1) & 7); };
@@ -446,7 +457,24 @@ void sparse_bf16_kernel(const SparseArgs a) {
   auto block_at = [&](int i) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane((int)list[i]); };
   using S0 = std::integral_constant<int, 0>;
   using S1 = std::integral_constant<int, 1>;
-  if (cnt > 0) tile_load(block_at(0), S0{});
+  // the first block's loads ahead of the list, on the guess that it is the first entry
+  const int* const entries = a.blocks + ((long)h * nqb + row) * a.keep;
+  const int first = __builtin_amdgcn_readfirstlane(entries[0]);
+  if ((uint32_t)first < (uint32_t)nkb) tile_load(first, S0{});
+  const int qrow = q0 + wave * 32 + (lane & 31);
+  bf16x8_t qf[HD / 16];
+#pragma unroll
+  for (int s = 0; s < HD / 16; ++s) {
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (qrow < L) u = *(const uint4*)(Q + qrow * tok + (s * 2 + hl) * 8);
+    qf[s] = __builtin_bit_cast(bf16x8_t, u);
+  }
+  const int cnt = __builtin_amdgcn_readfirstlane(
+      read_list(entries, a.keep, nkb, (uint32_t*)(lbase + SCRATCH), list, tid, 256));
+  if (cnt > 0 && block_at(0) != first) {
+    wait_vmcnt0_lgkmcnt0();  // the guess lands first
+    tile_load(block_at(0), S0{});
+  }
 
   f32x16_t o[HD / 32] = {};
   float mx = -FLT_MAX, l = 0.f;  // a finite start: keys whose scores are all -inf add nothing
@@ -586,9 +614,8 @@ constexpr int FD = 64, FQ = 16;
 __global__ __launch_bounds__(256) void sparse_f32_kernel(const SparseArgs a) {
   __shared__ float osh[4][FQ][FD + 4];
   __shared__ float2 ml[4][FQ];
-  __shared__ uint32_t mask[kSparseMaxKeyBlocks / 32];
+  __shared__ uint32_t scratch[kListScratch / 4];
   __shared__ uint16_t list[kSparseMaxKeyBlocks];
-  __shared__ int count;
   const SparseMeta& m = a.meta;
   const int nqb = m.qb_off[m.n_req];
   const int row = blockIdx.x / (kQB / FQ), h = blockIdx.y;
@@ -598,8 +625,8 @@ __global__ __launch_bounds__(256) void sparse_f32_kernel(const SparseArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 15, kq = lane >> 4;
   const long tok = (long)a.heads * FD, base = (long)m.off[r] * tok + (long)h * FD;
   const float *Q = (const float*)a.q + base, *K = (const float*)a.k + base, *V = (const float*)a.v + base;
-  const int cnt = read_list(a.blocks + ((long)h * nqb + row) * a.keep, a.keep, m.kb_off[r + 1] - m.kb_off[r], mask, list,
-                            &count, tid, 256);
+  const int cnt = read_list(a.blocks + ((long)h * nqb + row) * a.keep, a.keep, m.kb_off[r + 1] - m.kb_off[r], scratch,
+                            list, tid, 256);
   float4 q[4];
 #pragma unroll
   for (int c = 0; c < 4; ++c) q[c] = *(const float4*)(Q + min(q0 + lr, L - 1) * tok + c * 16 + kq * 4);
