@@ -332,10 +332,12 @@ dit_status dit_attention_select(const dit_batch* batch, int heads, int head_dim,
  * lists.  An entry outside [0, key blocks of the request) names none, one given
  * twice counts once, and the order of a list does not matter.  A query whose
  * list names no block gets O = 0.  K and V of blocks that no list names are not
- * read.  q, k, v, o, precisions and head_dim as for dit_attention; a request's
- * output bits do not depend on what it is packed with.  ws: device workspace of
- * at least dit_attention_sparse_workspace_size() bytes, 256-byte aligned; it may
- * be NULL where that size is 0.
+ * read.  q, k, v, o, precisions and head_dim as for dit_attention.  The order of
+ * a query's sums, and so its output bits, follow from its list alone, except that
+ * a DIT_BF16 call of at most 256 query blocks (times heads) with n_keep >= 8
+ * halves every list between two wave groups and adds their sums.  ws: device
+ * workspace of at least dit_attention_sparse_workspace_size() bytes, 256-byte
+ * aligned; it may be NULL where that size is 0.
  */
 dit_status dit_attention_sparse_workspace_size(const dit_batch* batch, int heads, int head_dim, int dtype, size_t* bytes);
 dit_status dit_attention_sparse(const dit_batch* batch, int heads, int head_dim, int dtype, const void* q, const void* k,

@@ -117,6 +117,48 @@ def test_sparse_attention_large_logits(dtype, d):
     _check(o, q, k, v, blocks, lens, dtype)
 
 
+@pytest.mark.parametrize("gain", [1.0, 16.0])
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_lists_of_every_length_up_to_nine(dtype, d, gain):
+    """Few query blocks with long lists of 0 .. 9 blocks, the ragged last one first, in between or last; any -1 between."""
+    torch = _torch()
+    b, lens = _batch([(32, 39, 5)])     # 1253 tokens: 10 query blocks, 20 key blocks, the last of 37 keys
+    heads = 2
+    q, k, v = _qkv(14, sum(lens), heads, d, dtype, gain=gain)
+    rng = np.random.default_rng(15)
+    blocks = np.full((heads, 10, 11), -1, np.int32)
+    for h in range(heads):
+        for i in range(10):
+            pick = rng.permutation(19)[:i]
+            if i:
+                pick[rng.integers(i)] = 19
+            if h == 0:
+                blocks[h, i, :i] = np.sort(pick)                 # ascending, as the selection writes them
+            else:
+                blocks[h, i, rng.permutation(11)[:i]] = pick
+    o = _run(b, heads, d, dtype, q.cuda(), k.cuda(), v.cuda(), torch.from_numpy(blocks).cuda())
+    _check(o, q, k, v, blocks, lens, dtype)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_infinite_scores_in_long_lists(dtype, d):
+    """As test_infinite_scores, with the keys of -inf in the first half of a list, in the second, in both."""
+    torch = _torch()
+    b, lens = _batch([(16, 64, 0)])
+    q, k, v = _qkv(16, 1024, 1, d, dtype)
+    q[:, 0, 0] = q[:, 0, 0].abs() + 0.5
+    k[0:512, 0, 0] = -float("inf")      # blocks 0 .. 7
+    blocks = np.array([[list(range(16)), list(range(8)) + [-1] * 8, [15 - i for i in range(16)], [7, 9] + [-1] * 14,
+                        list(range(8)) + [12] + [-1] * 7, [3] + [-1] * 15, [12] * 8 + [5] * 8, [15] * 16]], np.int32)
+    o = _run(b, 1, d, dtype, q.cuda(), k.cuda(), v.cuda(), torch.from_numpy(blocks).cuda()).double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        ref, mag = B.sparse_attention(*(x.double().numpy() for x in (q, k, v)), blocks, mag=True)
+    nan = np.r_[128:256, 640:768]
+    assert np.isnan(o[nan]).all() and np.isnan(ref[nan]).all()
+    keep = np.setdiff1d(np.arange(1024), nan)
+    assert (np.abs(o[keep] - ref[keep]) <= (4 * 2.0 ** -8 if dtype == "bf16" else 1e-4) * mag[keep]).all()
+
+
 @pytest.mark.parametrize("dtype,d", TYPES)
 def test_all_blocks_listed_is_dense_attention(dtype, d):
     torch = _torch()
