@@ -15,7 +15,8 @@
  *  - All tensors are device memory owned by the caller, dense and row-major.
  *    Element types: DIT_BF16 = bfloat16 (raw 16-bit storage), DIT_F32 = float.
  *  - No call allocates or frees device memory and none synchronises the host;
- *    all work is enqueued on `stream` (a hipStream_t; NULL = default stream)
+ *    all work is enqueued on `stream` (a hipStream_t; NULL = default stream),
+ *    which belongs to the calling thread's current device as all buffers do,
  *    and the call returns before it finishes.  Buffers must stay valid until
  *    the enqueued work completes.
  *  - Arguments are validated on the host before anything is enqueued; an
@@ -289,7 +290,8 @@ dit_status dit_quantize_fp8(int rows, int K, int block_rows, int dtype, const vo
  *    own rounding.
  * An output's bits depend on its row of X, its row of W, M and N, not on other
  * rows' values, and are the same on every call.  Codes 16-byte aligned, scales
- * 4-byte aligned, b and y aligned to their elements; M * N <= 2^36.
+ * 4-byte aligned, b and y aligned to their elements; M, N <= 2^30, M * N <= 2^36.
+ * y may not overlap the operands.
  */
 dit_status dit_linear_fp8(int M, int N, int K, const void* x_codes, const void* x_scales, const void* w_codes,
                           const void* w_scales, const void* b, int b_dtype, void* y, int out_dtype, void* stream);
@@ -319,7 +321,9 @@ dit_status dit_attention_query_blocks(const dit_batch* batch, int* n_blocks);
  * flags the key blocks that hold text rank before all others, in their order.
  * The lists are ascending, with -1 behind the last entry where a request has
  * fewer than n_keep blocks.  q, k as for dit_attention.  ws: device workspace of
- * at least dit_attention_select_workspace_size() bytes, 256-byte aligned.
+ * at least dit_attention_select_workspace_size() bytes, 256-byte aligned, written
+ * by every call: calls that may run at once (two streams, two captured graphs)
+ * need one each.
  */
 #define DIT_SELECT_TEXT 1
 dit_status dit_attention_select_workspace_size(const dit_batch* batch, int heads, int head_dim, int dtype, size_t* bytes);
@@ -337,7 +341,7 @@ dit_status dit_attention_select(const dit_batch* batch, int heads, int head_dim,
  * a DIT_BF16 call of at most 256 query blocks (times heads) with n_keep >= 8
  * halves every list between two wave groups and adds their sums.  ws: device
  * workspace of at least dit_attention_sparse_workspace_size() bytes, 256-byte
- * aligned; it may be NULL where that size is 0.
+ * aligned; it may be NULL where that size is 0.  o may not overlap k, v or blocks.
  */
 dit_status dit_attention_sparse_workspace_size(const dit_batch* batch, int heads, int head_dim, int dtype, size_t* bytes);
 dit_status dit_attention_sparse(const dit_batch* batch, int heads, int head_dim, int dtype, const void* q, const void* k,

@@ -697,7 +697,8 @@ dit_status noalloc_scratch(hipStream_t stream, void** out) {
 }
 // ---------------------------------------------------------------------------- 8-bit matrices
 constexpr int kFp8MaxK = 1 << 22;             // bytes of a row: offsets within 256 rows fit 32 bits
-constexpr double kFp8MaxOutputs = 1L << 36;   // blocks of the smallest tiles: fewer than 2^23
+constexpr int kFp8MaxSide = 1 << 30;          // of a product: a side rounded up to whole tiles fits 32 bits
+constexpr double kFp8MaxOutputs = 1L << 36;   // tiles and offsets within them fit 32 bits
 
 dit_status check_fp8_shape(int rows, int K, int block_rows) {
   if (rows < 0 || K <= 0) return fail(DIT_ERR_INVALID_ARG, "rows %d K %d", rows, K);
@@ -1097,6 +1098,7 @@ dit_status dit_linear_fp8(int M, int N, int K, const void* x_codes, const void* 
   if ((st = check_fp8_shape(M, K, 1))) return st;
   if (out_dtype != DIT_F32 && out_dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "out_dtype %d", out_dtype);
   if (b_dtype != DIT_F32 && b_dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "b_dtype %d", b_dtype);
+  if (M > kFp8MaxSide || N > kFp8MaxSide) return fail(DIT_ERR_UNSUPPORTED, "M %d or N %d exceeds 2^30", M, N);
   if ((double)M * N > kFp8MaxOutputs) return fail(DIT_ERR_UNSUPPORTED, "M %d x N %d exceeds 2^36", M, N);
   if (M == 0) return DIT_OK;
   if (!x_codes || !x_scales || !w_codes || !w_scales || !y)

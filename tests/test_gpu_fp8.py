@@ -264,3 +264,77 @@ def test_linear_fp8_every_kernel(M, N, K, out, cfg):
         got, ref, mag, ran = _large(M, N, K, out, "bf16" if off else "f32", M + N + K + off, off)
         assert "gemm_fp8_" + cfg in ran, ran
         _check_large(got, ref, mag, K, out)
+
+
+@pytest.mark.parametrize("block", [1, 128])
+def test_quantize_offsets_past_32_bits(block):
+    """More than 4 GiB of codes: the last rows against the reference, and equal rows at either end alike."""
+    torch = _torch()
+    rows, K = (1 << 20) + 129, 4097
+    x = torch.zeros((rows, K), dtype=torch.bfloat16, device="cuda")
+    x[-257:] = _matrix(21, 257, K, True).cuda()
+    nc, ns = dit.fp8_layout(rows, K, block)
+    assert nc > 1 << 32
+    q, s = torch.full((nc,), 9, dtype=torch.uint8, device="cuda"), torch.full((ns,), 9, dtype=torch.uint8, device="cuda")
+    dit.dit_quantize_fp8(rows, K, block, dit.DIT_BF16, x, q, s)
+    q, s = q.view(rows, -1), s.view(-(-rows // block), -1)
+    rq, rs = B.quantize_fp8(x[-257:].double().cpu().numpy(), block)   # rows of whole blocks: 257 = 129 + 128
+    assert np.array_equal(q[-257:].cpu().numpy(), rq) and np.array_equal(s[-rs.shape[0]:].cpu().numpy(), rs)
+    assert not q[:-257].any() and (s[:-rs.shape[0]] == 127).all()
+
+
+def _corners(M, N, K, out, seed):
+    """A product of random codes and scales, of any size that fits the card: its corners and middle against 64 bits."""
+    torch = _torch()
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    kb = -(-K // 128)
+    pitch = -(-kb // 4) * 4
+    ops = []
+    for rows, block in ((M, 1), (N, 128)):
+        nc, ns = dit.fp8_layout(rows, K, block)
+        q = torch.randint(0, 0x68, (nc,), generator=gen, device="cuda", dtype=torch.uint8)   # up to 60
+        q ^= torch.randint(0, 2, (nc,), generator=gen, device="cuda", dtype=torch.uint8) << 7
+        q.view(rows, kb * 128)[:, K:] = 0
+        s = torch.full((ns,), 127, dtype=torch.uint8, device="cuda")
+        s.view(-1, pitch)[:, :kb] = torch.randint(120, 130, (ns // pitch, kb), generator=gen, device="cuda", dtype=torch.uint8)
+        ops.append((q, s))
+    b = torch.randn((N,), generator=gen, device="cuda")
+    y = torch.empty((M * N + 64,), dtype=_dt(out)[0], device="cuda")
+    y[M * N:] = 55
+    dit.profile_start()
+    dit.dit_linear_fp8(M, N, K, ops[0][0], ops[0][1], ops[1][0], ops[1][1], b, dit.DIT_F32, y, _dt(out)[1])
+    torch.cuda.synchronize()
+    ran = set(dit.profile_stop())
+    assert (y[M * N:] == 55).all()
+    yv = y[:M * N].view(M, N)
+
+    def values(op, rows, lo, n, block):   # n rows from row lo
+        v = op[0].view(rows, -1)[lo:lo + n].contiguous().view(torch.float8_e4m3fn).double().view(n, kb, 128)
+        at = torch.arange(lo, lo + n, device="cuda") // block
+        e = op[1].view(-1, pitch)[at, :kb].long()
+        return (v * ((e + 1023 - 127) << 52).view(torch.float64)[:, :, None]).view(n, -1)[:, :K]
+    m, n = min(M, 260), min(N, 260)
+    for m0 in {0, M - m}:
+        for n0 in {0, N // 2 - n // 2, N - n}:
+            xv, wv = values(ops[0], M, m0, m, 1), values(ops[1], N, n0, n, 128)
+            ref = xv @ wv.t().contiguous() + b[n0:n0 + n].double()
+            mag = xv.abs() @ wv.abs().t().contiguous() + b[n0:n0 + n].double().abs()
+            _check_large(yv[m0:m0 + m, n0:n0 + n].double(), ref, mag, K, out)
+    return y.numel() * y.element_size(), ran
+
+
+@pytest.mark.parametrize("M,N,K,out,cfg", [
+    (66000, 33000, 400, "bf16", "256x256"), (33000, 33001, 130, "f32", "128x128"), (17, 1 << 27, 128, "bf16", "rows"),
+])
+def test_linear_fp8_offsets_past_32_bits(M, N, K, out, cfg):
+    """Outputs of more than 4 GiB (and codes of 17 GB in the last)."""
+    nbytes, ran = _corners(M, N, K, out, 22)
+    assert nbytes > 1 << 32 and "gemm_fp8_" + cfg in ran
+
+
+@pytest.mark.parametrize("M,N,out,cfg", [
+    (5, 40, "bf16", "rows"), (260, 300, "f32", "64x64"), (4100, 4100, "f32", "128x128"), (4090, 4090, "bf16", "256x256"),
+])
+def test_linear_fp8_longest_rows(M, N, out, cfg):
+    """K of 2^22, the most a row may hold."""
+    assert "gemm_fp8_" + cfg in _corners(M, N, 1 << 22, out, 23)[1]

@@ -340,6 +340,71 @@ def test_select_and_attend_at_the_largest_request():
     assert not o[:, 0, 1:].any()
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_sixteen_requests_and_lists_longer_than_any(dtype, d):
+    """The most requests a batch may hold, of 1 to 400 tokens, with lists of 2048 entries."""
+    torch = _torch()
+    reqs = [(1, 1 + r, (r * 37) % 200) for r in range(14)] + [(1, 1, 0), (20, 20, 0)]
+    b, lens = _batch(reqs)
+    q, k, v = _qkv(17, sum(lens), 2, d, dtype)
+    got = _select(b, 2, d, dtype, q.cuda(), k.cuda(), 2048, dit.DIT_SELECT_TEXT)
+    assert np.array_equal(got, _ref_select(q, k, lens, [r[2] for r in reqs], 2048))
+    blocks = _lists(18, lens, 2, 2048)
+    o = _run(b, 2, d, dtype, q.cuda(), k.cuda(), v.cuda(), torch.from_numpy(blocks).cuda())
+    _check(o, q, k, v, blocks, lens, dtype)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_most_heads(dtype, d):
+    """65535 heads of 2 tokens: every head's list and output."""
+    torch = _torch()
+    heads, b = 65535, _batch([(1, 2, 0)])[0]
+    gen = torch.Generator(device="cuda").manual_seed(19)
+    q, k, v = (torch.randn((2, heads, d), generator=gen, device="cuda").to(_dt(dtype)[0]) for _ in range(3))
+    blocks = _select(b, heads, d, dtype, q, k, 2)
+    assert (blocks == [0, -1]).all()
+    o = _run(b, heads, d, dtype, q, k, v, torch.from_numpy(blocks).cuda()).double()
+    q, k, v = (x.double() for x in (q, k, v))
+    p = torch.stack([(q * k[j]).sum(2) for j in range(2)], 2) / d ** 0.5   # [query, head, key]
+    S = max(q.abs().sum(2).max().item() * k.abs().max().item() / d ** 0.5, 1.0)
+    p = p.softmax(2)
+    ref = sum(p[:, :, j, None] * v[j] for j in range(2))
+    mag = sum(p[:, :, j, None] * v[j].abs() for j in range(2))
+    rel = 2 * (d + 3) * 2.0 ** -24 * S + 10 * 2.0 ** -24 + (3 * 2.0 ** -8 if dtype == "bf16" else 0)
+    assert ((o - ref).abs() <= rel * mag).all()
+
+
+@pytest.mark.parametrize("dtype,d,heads", [("bf16", 64, 261), ("bf16", 128, 131), ("f32", 64, 131)])
+def test_offsets_past_32_bits(dtype, d, heads):
+    """The largest request with q, k and v of more than 4 GiB each: the last heads' last query blocks."""
+    torch = _torch()
+    b, lens = _batch([(256, 256, 65536)])
+    T = lens[0]
+    gen = torch.Generator(device="cuda").manual_seed(20)
+    q, k, v = (torch.randn((T, heads, d), generator=gen, device="cuda", dtype=_dt(dtype)[0]) for _ in range(3))
+    assert q.numel() * q.element_size() > 1 << 32
+    blocks = torch.full((heads, T // 128, 3), -1, dtype=torch.int32, device="cuda")
+    blocks[-3:, -2:] = torch.tensor([2047, 5, 2046], dtype=torch.int32, device="cuda")
+    o = _run(b, heads, d, dtype, q, k, v, blocks)
+    assert not o[:, :-3].any() and not o[:-256].any()
+    pick = np.r_[5 * 64:6 * 64, 2046 * 64:2048 * 64]
+    qq = q[-256:, -3:].double().cpu().numpy()
+    kk, vv = (x[torch.from_numpy(pick).cuda(), -3:].double().cpu().numpy() for x in (k, v))
+    S = max(np.abs(qq[:, h]).sum(1).max() * np.abs(kk[:, h]).max() for h in range(3)) / d ** 0.5
+    rel = 2 * (d + 3) * 2.0 ** -24 * S + 200 * 2.0 ** -24 + (3 * 2.0 ** -8 if dtype == "bf16" else 0)
+    got = o[-256:, -3:].double().cpu().numpy()
+    for h in range(3):
+        p = np.exp(qq[:, h] @ kk[:, h].T / d ** 0.5)
+        p /= p.sum(1, keepdims=True)
+        assert (np.abs(got[:, h] - p @ vv[:, h]) <= rel * (p @ np.abs(vv[:, h]))).all()
+    # the selection over the same tensors: the last query blocks of the last heads
+    lists = _select(b, heads, d, dtype, q, k, 40)
+    km = [k[:, h].double().view(2048, 64, d).mean(1) for h in range(heads - 3, heads)]
+    for i, h in enumerate(range(heads - 3, heads)):
+        s = (q[-128:, h].double().mean(0) * km[i]).sum(1)
+        assert np.array_equal(lists[h, -1], np.sort(s.topk(40).indices.cpu().numpy()))
+
+
 # ---------------------------------------------------------------------------- together
 def _layer(b, T, heads, d, keep, bufs, stream=None):
     """One attention layer in 8 bits, as a program chains the calls: x -> codes -> q, k, v -> lists -> attention -> codes -> y."""
@@ -419,3 +484,48 @@ def test_layer_in_8_bits_eager_and_captured(reqs, keep):
         torch.cuda.synchronize()
         assert torch.equal(w["y"], want[i])
         assert torch.equal(eager(inputs[(i + 1) % 3]), want[(i + 1) % 3])
+
+
+def test_two_layers_at_once():
+    """Two chains in flight on two streams, each with buffers of its own, give the bits that each gives alone."""
+    torch = _torch()
+    heads, d, keep = 4, 64, 6
+    b, lens = _batch([(24, 24, 30), (9, 9, 0)])
+    T, H = sum(lens), heads * d
+    n = dit.attention_select_workspace_size(b, heads, d, dit.DIT_BF16)
+    sets = []
+    for seed in (30, 31):
+        w = {"ws": torch.empty(n, dtype=torch.uint8, device="cuda")}
+        w["x"] = torch.from_numpy(synth.normal(seed, "x", (T, H))).to(torch.bfloat16).cuda()
+        nc, ns = dit.fp8_layout(T, H, 1)
+        w["xq"], w["xs"] = torch.empty(nc, dtype=torch.uint8, device="cuda"), torch.empty(ns, dtype=torch.uint8, device="cuda")
+        for nm in "qkvo":
+            wt = torch.from_numpy(synth.normal(seed, "w" + nm, (H, H), std=H ** -0.5)).to(torch.bfloat16).cuda()
+            nc, ns = dit.fp8_layout(H, H, 128)
+            w["w" + nm], w["s" + nm] = torch.empty(nc, dtype=torch.uint8, device="cuda"), torch.empty(ns, dtype=torch.uint8, device="cuda")
+            dit.dit_quantize_fp8(H, H, 128, dit.DIT_BF16, wt, w["w" + nm], w["s" + nm])
+            w["b" + nm] = torch.from_numpy(synth.normal(seed, "b" + nm, (H,))).to(torch.bfloat16).cuda()
+        for nm in "qkv":
+            w[nm] = torch.empty((T, heads, d), dtype=torch.bfloat16, device="cuda")
+        w["o"] = torch.empty((T, H), dtype=torch.bfloat16, device="cuda")
+        w["y"] = torch.empty((T, H), dtype=torch.float32, device="cuda")
+        w["blocks"] = torch.empty((heads, dit.attention_query_blocks(b), keep), dtype=torch.int32, device="cuda")
+        sets.append(w)
+    alone = []
+    for w in sets:
+        _layer(b, T, heads, d, keep, w)
+        torch.cuda.synchronize()
+        alone.append({k: w[k].clone() for k in ("blocks", "o", "y")})
+        assert torch.isfinite(w["y"]).all()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(20):
+        for w in sets:
+            for k in ("blocks", "o", "y"):
+                w[k].zero_()
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for w, s in zip(sets, streams):
+                _layer(b, T, heads, d, keep, w, s)
+        torch.cuda.synchronize()
+        for w, ref in zip(sets, alone):
+            assert all(torch.equal(w[k], ref[k]) for k in ref)

@@ -62,6 +62,14 @@ def test_linear_fp8_refusals():
     dit.dit_linear_fp8(0, 8, 64, 0, 0, 0, 0, 0, BF, 0, BF, 0)
 
 
+def test_linear_fp8_refuses_sides_and_outputs_past_its_offsets():
+    def err(M, N):
+        return _err(dit.dit_linear_fp8, M, N, 64, P, P, P, P, P, BF, P, BF, 0)
+    top = (1 << 31) - 1
+    assert err(1, top) == UNS and err(top, 1) == UNS and err(1, (1 << 30) + 1) == UNS and err((1 << 30) + 1, 1) == UNS
+    assert err(1 << 18, (1 << 18) + 1) == UNS and err(65537, 1 << 20) == UNS
+
+
 def _batch(*lens):
     """Requests of the given joint lengths, one image token and the rest text."""
     return dit.Batch([1] * len(lens), [1] * len(lens), [x - 1 for x in lens])
