@@ -40,7 +40,9 @@ __device__ __forceinline__ long key_mean_at(const SparseMeta& m, int hd, int h, 
 
 // Block (key or query block, 512 columns of [heads, head_dim]): its mean, 64
 // bits.  A wave reads 1 KB of a token's row at a time and takes every eighth
-// token; the waves' sums meet in LDS.  Every element of Q and K is read once.
+// token; the waves' sums meet in LDS.  Every element of Q and K is read once, and
+// that bounds it: 155 us for 66048 tokens of 24 heads of 128, 5.2 TB/s, what a large
+// copy reaches (4.8, reads and writes).
 template <typename T>
 __global__ __launch_bounds__(512) void block_means_kernel(const T* __restrict__ q, const T* __restrict__ k, int heads,
                                                           int hd, const SparseMeta m, double* __restrict__ qm,
@@ -183,6 +185,10 @@ __device__ __forceinline__ uint32_t halve_scores(const uint32_t* key, int want) 
 // kept in LDS as order-preserving integers, high and low words apart.  Then a
 // wave takes a query block, 64 NV scores in registers, and finds the keep-th
 // largest: by the high words, and by the low words among equal ones.
+// 516 x 1032 scores of 24 heads of 128: 137 us, of which the matrix cores need 55
+// (59 TFLOP/s); the rest is the search's counting, one block a CU (208 us with the
+// key means in rows, 162 with a search by bits alone).  Small calls are latency:
+// 35 x 70 scores of 24 heads about 6 us.
 template <int HD, int NV, int R, int NW>
 __global__ __launch_bounds__(NW * 64) void select_blocks_kernel(const double* __restrict__ qm,
                                                                 const double* __restrict__ km, const SparseMeta m,
@@ -289,14 +295,18 @@ void launch_select(const double* qm, const double* km, int heads, const SparseMe
 }
 
 // Query blocks per thread block: 16, which fill the matrix cores' columns; 4 where
-// that leaves CUs idle and the scores are few; 8 where 16 rows of scores exceed
-// LDS.
+// the scores are few (under 2^19), which spreads them over more CUs; 8 where 16
+// rows of scores exceed LDS.  Both launches of a call in us, 4 against 16 (query
+// blocks times heads x key blocks): 840 x 70 14.4 against 20.4, 1512 x 125 20.5
+// against 25.9, 4032 x 125 38.2 against 40.2; 8064 x 125 78.1 against 73.6, 3168 x
+// 264 69.0 against 61.1, 12384 x 1032 453 against 302 (means 155 of it).  Past 320
+// key blocks, 516 x 344 28.8 against 33.9 and 1032 x 344 equal: not worth a kernel.
 template <int HD>
 void launch_select(const double* qm, const double* km, int heads, const SparseMeta& m, int text_first, int keep, int* out,
                    hipStream_t s) {
   int n = 0;
   for (int r = 0; r < m.n_req; ++r) n = std::max(n, m.kb_off[r + 1] - m.kb_off[r]);
-  const bool few = (long)m.qb_off[m.n_req] * heads < 512 * 16;
+  const bool few = (long)m.qb_off[m.n_req] * heads * n < 1 << 19;
   if (n <= 128) {
     if (few) launch_select<HD, 2, 4, 8>(qm, km, heads, m, text_first, keep, out, s);
     else launch_select<HD, 2, 16, 4>(qm, km, heads, m, text_first, keep, out, s);
@@ -400,6 +410,13 @@ __device__ __forceinline__ void read_ahead() {
 // (ds_read_b64_tr_b16: 16 lanes take a block of 4 keys x 16 dimensions, each lane
 // the 4 keys of one dimension), so no copy of V is made and the keys a lane gets
 // are those whose probabilities it holds.
+//
+// 16896 tokens, 24 heads of 128, lists of 33: 450 us, 970 TFLOP/s; three requests of
+// 589 + 1357 + 4429 tokens, 12 heads of 64, lists of 16: 33 us.  The matrix cores are
+// busy half of the time, vector arithmetic (an exponential, a multiply-add, a
+// rounding and a sum per score) for most of the other; neither fewer LDS reads (64
+// queries a wave, head_dim 64: 254 -> 266 us at 16896 tokens) nor a fourth wave per
+// SIMD (247 -> 245) helps.
 //
 // KG = 2: two such groups of 4 waves halve the list between them, each with LDS
 // stages of its own; the second hands its O, max and sum to the first through LDS
