@@ -600,59 +600,175 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void fp8_ring_kernel(const Fp8Prob
   }
 }
 
+// ---------------------------------------------------------------- small tiles, K shared out to the waves
+// BM x BN = 16 FM x 16 FN outputs per block, NW waves that share out the K tiles: a
+// wave multiplies all rows and columns of its K tiles, which nobody else reads, so
+// the waves need no barrier until their sums meet in LDS, in wave order.  K tiles
+// arrive by direct-to-LDS loads in two stages of each wave's own (loads to registers,
+// 64 bytes of 16 rows each, reach half the rate).  As above W's rows are dealt out to
+// the fragments, and a lane ends with 4 FN neighbouring columns of a row.  For outputs
+// that fill one round of CUs or less: what a CU loads bounds these products (60 - 85
+// bytes per ns), and smaller tiles spread it over more CUs.  4 waves (8: 4 - 25% slower
+// past one round, where fewer blocks fit a CU).  64 x 1536 x 6144: 6.4 us.
+template <bool F32, int FM, int FN, int NW>
+__global__ __launch_bounds__(NW * 64) void fp8_split_kernel(const Fp8Problem p) {
+  constexpr int BM = FM * 16, BN = FN * 16, ROWB = 128, TILE = (BM + BN) * ROWB;
+  constexpr int LOADS = (BM + BN) / 8 + FM + 1;  // of a K tile
+  __shared__ uint4 lds[NW * 2 * TILE / 16];      // [wave][stage][X's rows, then W's]; then the waves' sums
+  static_assert(FM <= NW && FM * FN * 1024 <= 2 * TILE && BN <= 128, "tile config");
+  const int tn = (p.N + BN - 1) / BN, tm = (p.M + BM - 1) / BM;
+  const int id = (int)(blockIdx.y << kRingRowLog2) + xcd_remap(blockIdx.x, gridDim.x);
+  if (id >= tm * tn) return;
+  int im, in;
+  tile_of(id, tm, tn, im, in);
+  const int m0 = im * BM, n0 = in * BN, Kp = p.kb * kFp8Block;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15;
+  char* const lbase = (char*)lds + wv * 2 * TILE;
+  auto swz = [](int row, int c) { return c ^ ((row >> 1) & 7); };
+  // loads of 8 rows: of X, and of either half of a fragment of W
+  const int row = lane >> 3;
+  uint32_t xo[2], wo[2], so[FM];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = h * 8 + row, c = swz(r, lane & 7) * 16;
+    xo[h] = row * (uint32_t)Kp + c;
+    wo[h] = (uint32_t)((r >> 2) * (4 * FN) + (r & 3)) * (uint32_t)Kp + c;
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i) so[i] = (i * 16 + lr) * (uint32_t)p.pitch;
+  // rows past the last one read as zeros, and so do K tiles
+  auto rows = [&](const uint8_t* base, int r0, int most, int n, int pitch) __attribute__((always_inline)) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (long)r0 * pitch), (short)0,
+                                             __builtin_amdgcn_readfirstlane(min(n - r0, most) * pitch), kBufferWord3);
+  };
+  int sx[2][FM], sw[2];
+  auto load = [&](int kt, auto stc) __attribute__((always_inline)) {
+    constexpr int st = decltype(stc)::value;
+    const bool in = kt < p.kb;
+    const __amdgpu_buffer_rsrc_t rx = rows(p.x, m0, in ? BM : 0, p.M, Kp), rw = rows(p.w, n0, in ? BN : 0, p.N, Kp);
+    const __amdgpu_buffer_rsrc_t rsx = rows(p.xs, m0, in ? BM : 0, p.M, p.pitch);
+    const __amdgpu_buffer_rsrc_t rsw = rows(p.ws, n0 >> 7, in ? 1 : 0, (p.N + 127) >> 7, p.pitch);
+#pragma unroll
+    for (int i = 0; i < BM / 8; ++i) {
+      const int vo = (int)xo[i & 1], at = kt * ROWB + i * 8 * Kp;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (__attribute__((address_space(3))) void*)(lbase + st * TILE + i * 1024), 16, vo,
+                                               at, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < BN / 8; ++i) {
+      const int vo = (int)wo[i & 1], at = kt * ROWB + (i >> 1) * 4 * Kp;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rw, (__attribute__((address_space(3))) void*)(lbase + st * TILE + (BM / 8 + i) * 1024), 16, vo, at, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) sx[st][i] = __builtin_amdgcn_raw_buffer_load_b8(rsx, so[i], kt, 0);
+    sw[st] = __builtin_amdgcn_raw_buffer_load_b8(rsw, 0, kt, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int fa[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) fa[h] = lr * ROWB + swz(lr, (lane >> 4) + 4 * h) * 16;
+  auto frag = [&](int at) __attribute__((always_inline)) {
+    const i32x4_t lo = __builtin_bit_cast(i32x4_t, *(const uint4*)(lbase + at + fa[0]));
+    const i32x4_t hi = __builtin_bit_cast(i32x4_t, *(const uint4*)(lbase + at + fa[1]));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  f32x4_t acc[FM][FN] = {};
+  auto step = [&](int kt, auto stc) __attribute__((always_inline)) {
+    constexpr int st = decltype(stc)::value;
+    wait_vmcnt<LOADS>();  // all but the next K tile's loads
+    __builtin_amdgcn_sched_barrier(0);
+    i32x8_t x[FM], w[FN];
+    int xs[FM], ws[FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      x[i] = frag(st * TILE + i * 16 * ROWB);
+      xs[i] = sx[st][i];
+    }
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      w[j] = frag(st * TILE + (BM + j * 16) * ROWB);
+      ws[j] = sw[st];
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): read, before the K tile after the next arrives here
+    __builtin_amdgcn_sched_barrier(0);
+    load(kt + 2 * NW, stc);
+    multiply<F32, FM, FN>(x, w, xs, ws, acc);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  using S0 = std::integral_constant<int, 0>;
+  using S1 = std::integral_constant<int, 1>;
+  load(wv, S0{});
+  load(wv + NW, S1{});
+#pragma unroll 1
+  for (int k = wv; k < p.kb; k += 2 * NW) {
+    step(k, S0{});
+    step(k + NW, S1{});
+  }
+  wait_vmcnt<0>();
+  uint4* const sums = lds + lane;
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) sums[wv * (2 * TILE / 16) + (i * FN + j) * 64] = __builtin_bit_cast(uint4, acc[i][j]);
+  __syncthreads();
+  if (wv >= FM) return;  // wave i finishes rows 16 i ..
+  const int m = m0 + wv * 16 + lr, n = n0 + (lane >> 4) * (4 * FN);
+  if (m >= p.M || n >= p.N) return;
+  float v[4 * FN];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) {
+    f32x4_t s = __builtin_bit_cast(f32x4_t, sums[(wv * FN + j) * 64]);
+#pragma unroll
+    for (int g = 1; g < NW; ++g) s += __builtin_bit_cast(f32x4_t, sums[g * (2 * TILE / 16) + (wv * FN + j) * 64]);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[j * 4 + r] = s[r] + (n + j * 4 + r < p.N ? bias_at(p, n + j * 4 + r) : 0.f);
+  }
+  store_columns<F32, 4 * FN>((char*)p.y + ((long)m * p.N + n) * (F32 ? 4 : 2), v, p.N - n);
+}
+
 // ---------------------------------------------------------------- few rows
 __device__ __forceinline__ i32x8_t load32(const uint8_t* p) {
   return __builtin_shufflevector(((const i32x4_t*)p)[0], ((const i32x4_t*)p)[1], 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Up to 16 MF rows of X against 16 columns per block: W is read once, straight
-// from memory to registers, and the block's waves share out the K tiles, two in
-// flight each.  Their sums meet in LDS in wave order.  4 x 9216 x 1536: 6 us with the
-// launch (14 MB of W, 2.4 TB/s), of which the host's call is 4.4.
-template <bool F32, int MF, int NW>
-__global__ __launch_bounds__(NW * 64) void fp8_rows_kernel(const Fp8Problem p) {
-  __shared__ f32x4_t part[NW][MF][64];
+// Up to 16 rows of X against 16 columns per block: W is read once, straight from
+// memory to registers, and the block's waves share out the K tiles, two in flight
+// each.  Their sums meet in LDS in wave order.  4 x 9216 x 1536: 6 us with the launch
+// (14 MB of W, 2.4 TB/s).
+template <bool F32>
+__global__ __launch_bounds__(512) void fp8_rows_kernel(const Fp8Problem p) {
+  constexpr int NW = 8, U = 2;
+  __shared__ f32x4_t part[NW][64];
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int strip = (int)(blockIdx.y << kRingRowLog2) + (int)blockIdx.x;
-  if (strip >= ((uint32_t)p.N + 15) / 16) return;
-  const int lr = lane & 15, n0 = strip * 16, Kp = p.kb * kFp8Block;
+  const int lr = lane & 15, n0 = blockIdx.x * 16, Kp = p.kb * kFp8Block;
   const uint8_t* const w = p.w + (long)min(n0 + lr, p.N - 1) * Kp + (lane >> 4) * 32;
   const uint8_t* const ws = p.ws + (long)(n0 >> 7) * p.pitch;
-  const uint8_t *x[MF], *xs[MF];
-#pragma unroll
-  for (int i = 0; i < MF; ++i) {
-    const int m = min(i * 16 + lr, p.M - 1);
-    x[i] = p.x + (long)m * Kp + (lane >> 4) * 32;
-    xs[i] = p.xs + (long)m * p.pitch;
-  }
-  f32x4_t acc[MF][1] = {};
-  constexpr int U = 2;
+  const uint8_t* const x = p.x + (long)min(lr, p.M - 1) * Kp + (lane >> 4) * 32;
+  const uint8_t* const xs = p.xs + (long)min(lr, p.M - 1) * p.pitch;
+  f32x4_t acc[1][1] = {};
   for (int k0 = wv; k0 < p.kb; k0 += NW * U) {
-    i32x8_t wf[U], xf[U][MF];
-    int sw[U], sx[U][MF];
+    i32x8_t wf[U], xf[U];
+    int sw[U], sx[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int kt = min(k0 + u * NW, p.kb - 1);  // past the end: loaded again, not multiplied
       wf[u] = load32(w + (long)kt * 128);
       sw[u] = ws[kt];
-#pragma unroll
-      for (int i = 0; i < MF; ++i) {
-        xf[u][i] = load32(x[i] + (long)kt * 128);
-        sx[u][i] = xs[i][kt];
-      }
+      xf[u] = load32(x + (long)kt * 128);
+      sx[u] = xs[kt];
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (k0 + u * NW < p.kb) multiply<F32, MF, 1>(xf[u], &wf[u], sx[u], &sw[u], acc);
+      if (k0 + u * NW < p.kb) multiply<F32, 1, 1>(&xf[u], &wf[u], &sx[u], &sw[u], acc);
   }
-#pragma unroll
-  for (int i = 0; i < MF; ++i) part[wv][i][lane] = acc[i][0];
+  part[wv][lane] = acc[0][0];
   __syncthreads();
-  if (wv >= MF) return;  // wave i finishes rows 16 i ..
-  f32x4_t s = part[0][wv][lane];
+  if (wv > 0) return;
+  f32x4_t s = part[0][lane];
 #pragma unroll
-  for (int g = 1; g < NW; ++g) s += part[g][wv][lane];
-  const int m = wv * 16 + lr, n = n0 + (lane >> 4) * 4;
+  for (int g = 1; g < NW; ++g) s += part[g][lane];
+  const int m = lr, n = n0 + (lane >> 4) * 4;
   if (m >= p.M) return;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -668,37 +784,46 @@ __global__ __launch_bounds__(NW * 64) void fp8_rows_kernel(const Fp8Problem p) {
 
 // Which kernel a product takes: the one whose modelled time is least.  In
 // microseconds, rounds of 256 tiles times (a fixed part + a part per K tile of
-// 128), fitted to 25 shapes (M 1 - 8629, N 1536 - 16384, K 256 - 16384; it picks
-// the fastest of the four or one within 8% of it on all of them):
-//   64 x 64      589 x 1536 x 6144 15.2 (128 x 128: 28.9), 589 x 1536 x 1536 6.6
-//   128 x 128    4429 x 1536 x 1536 20.3 (64: 34.3, 256: 25.7), 589 x 6144 x 1536 12.1
+// 128), and no less than reading W takes; fitted to 76 shapes (M 1 - 16896, N 33 -
+// 262144, K 64 - 65536; it picks the fastest or one within 13% of it on all of them).
+// Up to 16 rows there is one more, up to a W of 32 MB.  Measured, in us with the
+// launch, bf16 output, these first ones with W not in the caches:
+//   rows         4 x 9216 x 1536 6.1 (16 x 32: 7.1), 16 x 1536 x 6144 8.8 (9.9), but
+//                16 x 16384 x 4096 22 (18.7), where X's share of the traffic counts
+//   16 x 32      64 x 1536 x 6144 6.4 (32 x 32: 7.6, 64 x 64: 13.2)
+//   32 x 32      128 x 1536 x 6144 7.9 (16 x 32: 9.6, 32 x 64: 9.8)
+//   32 x 64      200 x 1536 x 6144 10.0 (32 x 32: 12.6, 64 x 64: 13.5)
+//   64 x 64      589 x 1536 x 6144 14.8 (32 x 64: 21.5, 128 x 128: 28.5), 589 x 1536 x 1536 6.4
+//   128 x 128    4429 x 1536 x 1536 20.3 (64: 34.3, 256: 25.7), 333 x 6144 x 1536 10.7 (64: 15.6)
 //   256 x 256    4429 x 6144 x 1536 47 (128: 65); a launch of one round leaves the
 //                chip its clock, hence two lines
-//   rows         16 x 1536 x 6144 8.5 (64: 12.7), but 16 x 16384 x 4096 21.7 (64: 12.9),
-//                where X's share of the traffic counts
-enum Fp8Cfg { FP8_ROWS, FP8_64, FP8_128, FP8_256 };
+enum Fp8Cfg { FP8_ROWS, FP8_16X32, FP8_32X32, FP8_32X64, FP8_64, FP8_128, FP8_256 };
 static Fp8Cfg pick(int M, int N, int K, int out_dtype) {
   const double kt = fp8_k_blocks(K);
   const bool f32 = out_dtype == DIT_F32;
-  auto rounds = [&](int t) { return ceil(ceil((double)M / t) * ceil((double)N / t) / 256.0); };
+  if (M <= 16 && N * kt * 128 <= 1 << 25) return FP8_ROWS;
+  auto rounds = [&](int bm, int bn) { return ceil(ceil((double)M / bm) * ceil((double)N / bn) / 256.0); };
   Fp8Cfg cfg = FP8_64;
-  double best = 2.0 + rounds(64) * (1.5 + (f32 ? 0.36 : 0.235) * kt);
+  double best = 2.0 + rounds(64, 64) * (1.5 + (f32 ? 0.36 : 0.235) * kt);
   auto offer = [&](Fp8Cfg c, double us) {
     if (us < best) {
       best = us;
       cfg = c;
     }
   };
-  offer(FP8_128, 2.0 + rounds(128) * (2.75 + (f32 ? 1.07 : 0.547) * kt));
+  const double memory = 2.9 + N * kt * 128 / 7e6;
+  offer(FP8_16X32, fmax(2.9 + rounds(16, 32) * (0.7 + (f32 ? 0.065 : 0.06) * kt), memory));
+  offer(FP8_32X32, fmax(2.9 + rounds(32, 32) * (1.15 + (f32 ? 0.095 : 0.083) * kt), memory));
+  offer(FP8_32X64, fmax(1.7 + rounds(32, 64) * (3.2 + (f32 ? 0.16 : 0.145) * kt), memory));
+  offer(FP8_128, 2.0 + rounds(128, 128) * (2.75 + (f32 ? 1.07 : 0.547) * kt));
   // offsets within a tile of 256 output rows fit 32 bits up to 2^21 columns
   if (!f32 && kt >= kMinKTiles256 && N <= 1 << 21)
-    offer(FP8_256, rounds(256) <= 1 ? 13.5 + 1.02 * kt : rounds(256) * (7.0 + 1.45 * kt));
-  if (M <= 32) offer(FP8_ROWS, 3.5 + fmax(ceil(N / 16.0) * kt * 2048 * (1 + M / 16.0) / 7e6, kt * (0.045 + 0.004 * M)));
+    offer(FP8_256, rounds(256, 256) <= 1 ? 13.5 + 1.02 * kt : rounds(256, 256) * (7.0 + 1.45 * kt));
   return cfg;
 }
 
 const char* gemm_fp8_config_name(int M, int N, int K, int out_dtype) {
-  static const char* names[] = {"gemm_fp8_rows", "gemm_fp8_64x64", "gemm_fp8_128x128", "gemm_fp8_256x256"};
+  static const char* names[] = {"gemm_fp8_rows", "gemm_fp8_16x32", "gemm_fp8_32x32", "gemm_fp8_32x64", "gemm_fp8_64x64", "gemm_fp8_128x128", "gemm_fp8_256x256"};
   return names[pick(M, N, K, out_dtype)];
 }
 
@@ -713,13 +838,21 @@ static void launch_ring(const Fp8Problem& p, hipStream_t s) {
   hipLaunchKernelGGL((fp8_ring_kernel<F32, BM, BN, WM, WN, KG, ST>), grid, dim3(WM * WN * KG * 64), 0, s, p);
 }
 
+template <bool F32, int FM, int FN>
+static void launch_split(const Fp8Problem& p, hipStream_t s) {
+  constexpr int NW = 4, BM = FM * 16, BN = FN * 16;
+  const dim3 grid = ring_grid((long)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN));
+  hipLaunchKernelGGL((fp8_split_kernel<F32, FM, FN, NW>), grid, dim3(NW * 64), 0, s, p);
+}
+
 template <bool F32>
 static void launch_small(Fp8Cfg cfg, const Fp8Problem& p, hipStream_t s) {
-  const dim3 strips = ring_grid(((long)p.N + 15) / 16);
-  if (cfg == FP8_64) launch_ring<F32, 64, 64, 2, 2, 2, 4>(p, s);
-  else if (cfg == FP8_128) launch_ring<F32, 128, 128, 2, 4, 1, 4>(p, s);
-  else if (p.M <= 16) hipLaunchKernelGGL((fp8_rows_kernel<F32, 1, 8>), strips, dim3(512), 0, s, p);
-  else hipLaunchKernelGGL((fp8_rows_kernel<F32, 2, 8>), strips, dim3(512), 0, s, p);
+  if (cfg == FP8_ROWS) hipLaunchKernelGGL((fp8_rows_kernel<F32>), dim3((p.N + 15) / 16), dim3(512), 0, s, p);
+  else if (cfg == FP8_16X32) launch_split<F32, 1, 2>(p, s);
+  else if (cfg == FP8_32X32) launch_split<F32, 2, 2>(p, s);
+  else if (cfg == FP8_32X64) launch_split<F32, 2, 4>(p, s);
+  else if (cfg == FP8_64) launch_ring<F32, 64, 64, 2, 2, 2, 4>(p, s);
+  else launch_ring<F32, 128, 128, 2, 4, 1, 4>(p, s);
 }
 
 hipError_t launch_gemm_fp8(int M, int N, int K, const void* x, const void* xs, const void* w, const void* ws,

@@ -253,8 +253,10 @@ def test_linear_fp8_256x256(M, N, K, bias, off):
 
 
 @pytest.mark.parametrize("M,N,K,out,cfg", [
-    (1, 4100, 513, "f32", "rows"), (16, 1000, 6000, "bf16", "rows"), (31, 77, 1300, "f32", "rows"), (32, 48, 128, "bf16", "rows"),
-    (33, 4001, 300, "bf16", "64x64"), (589, 1536, 6144, "f32", "64x64"), (300, 999, 2000, "bf16", "64x64"), (20, 20000, 700, "bf16", "64x64"),
+    (1, 4100, 513, "f32", "rows"), (16, 1000, 6000, "bf16", "rows"), (13, 15, 128, "f32", "rows"), (16, 9000, 4000, "f32", "16x32"),
+    (31, 77, 1300, "f32", "16x32"), (32, 48, 128, "bf16", "16x32"),
+    (70, 1700, 6000, "bf16", "32x32"), (130, 1530, 2000, "f32", "32x32"), (300, 999, 2000, "bf16", "32x64"), (199, 1501, 900, "f32", "32x64"),
+    (33, 4001, 300, "bf16", "64x64"), (589, 1536, 6144, "f32", "64x64"), (20, 20000, 700, "bf16", "64x64"),
     (4429, 1530, 1536, "bf16", "128x128"), (4429, 1530, 900, "f32", "128x128"), (4000, 3999, 100, "bf16", "128x128"),
     (4000, 4001, 257, "f32", "128x128"), (4429, 6144, 1500, "bf16", "256x256"),
 ])
@@ -324,16 +326,18 @@ def _corners(M, N, K, out, seed):
 
 
 @pytest.mark.parametrize("M,N,K,out,cfg", [
-    (66000, 33000, 400, "bf16", "256x256"), (33000, 33001, 130, "f32", "128x128"), (17, 1 << 27, 128, "bf16", "rows"),
+    (66000, 33000, 400, "bf16", "256x256"), (33000, 33001, 130, "f32", "128x128"), (17, 1 << 27, 128, "bf16", "128x128"),
+    (1, (1 << 28) + 5, 128, "bf16", "16x32"),   # more blocks than a row of the grid holds
 ])
 def test_linear_fp8_offsets_past_32_bits(M, N, K, out, cfg):
-    """Outputs of more than 4 GiB (and codes of 17 GB in the last)."""
+    """Outputs of more than 4 GiB, codes of 17 and 34 GB."""
     nbytes, ran = _corners(M, N, K, out, 22)
-    assert nbytes > 1 << 32 and "gemm_fp8_" + cfg in ran
+    assert max(nbytes, N * K) > 1 << 32 and "gemm_fp8_" + cfg in ran
 
 
 @pytest.mark.parametrize("M,N,out,cfg", [
-    (5, 40, "bf16", "rows"), (260, 300, "f32", "64x64"), (4100, 4100, "f32", "128x128"), (4090, 4090, "bf16", "256x256"),
+    (5, 7, "bf16", "rows"), (5, 40, "bf16", "16x32"), (260, 300, "f32", "16x32"), (256, 900, "f32", "32x32"), (500, 1000, "bf16", "32x64"),
+    (1000, 1000, "bf16", "64x64"), (4000, 4000, "f32", "128x128"), (4090, 4090, "bf16", "256x256"),
 ])
 def test_linear_fp8_longest_rows(M, N, out, cfg):
     """K of 2^22, the most a row may hold."""
