@@ -28,28 +28,33 @@ __device__ __forceinline__ uint32_t finite_mag(float v) {
   return m < 0x7f800000 ? m : 0;
 }
 
-// 8 consecutive elements x[0 .. 7], of which the first n exist (others 0).
-// VEC: the row is 16-byte aligned and n is 8 or 0.
-template <typename T, bool VEC>
+// 16 bytes at any element's address
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Bytes16 {
+  uint32_t w[4];
+};
+
+// 8 consecutive elements x[0 .. 7], of which the first n exist (others 0).  Whole
+// ones are loaded 16 bytes at a time wherever they lie: a row of odd length starts
+// anywhere (5152 x 3186 bf16 12.3 us, element by element 24.5).
+template <typename T>
 __device__ __forceinline__ void load8(const T* x, int n, float* v) {
-  if constexpr (VEC) {
+  if (n == 8) {
+    const Bytes16<T>* const p = (const Bytes16<T>*)x;
     if constexpr (sizeof(T) == 2) {
-      uint4 u = make_uint4(0, 0, 0, 0);
-      if (n > 0) u = *(const uint4*)x;
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      const Bytes16<T> u = p[0];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000);
+        v[2 * i] = __uint_as_float(u.w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(u.w[i] & 0xffff0000);
       }
     } else {
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-      if (n > 0) {
-        a = ((const float4*)x)[0];
-        b = ((const float4*)x)[1];
+      const Bytes16<T> a = p[0], b = p[1];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[i] = __uint_as_float(a.w[i]);
+        v[4 + i] = __uint_as_float(b.w[i]);
       }
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-      v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
     }
   } else {
 #pragma unroll
@@ -68,7 +73,7 @@ __device__ __forceinline__ uint2 codes8(const float* v, float inv) {
 
 // 1 x 128: a wave takes 512 elements of a row, 8 per lane; 16 lanes share a
 // scale and the wave's four scales leave as one word.
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const T* __restrict__ x, long rows, int K, int Kp,
                                                             int chunks, uint8_t* __restrict__ q,
                                                             uint32_t* __restrict__ s) {
@@ -78,7 +83,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const T* __restrict_
   const long row = unit / chunks;
   const int c = (int)(unit - row * chunks), k = c * 512 + lane * 8;
   float v[8];
-  load8<T, VEC>(x + row * K + k, min(max(K - k, 0), 8), v);
+  load8<T>(x + row * K + k, min(max(K - k, 0), 8), v);
   uint32_t a = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) a = max(a, finite_mag(v[i]));
@@ -93,7 +98,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const T* __restrict_
 }
 
 // 128 x 128: a block of threads takes one tile, 16 lanes a row, 8 rows each
-template <typename T, bool VEC>
+template <typename T>
 __global__ __launch_bounds__(256) void quantize_tiles_kernel(const T* __restrict__ x, long rows, int K, int Kp, int kb,
                                                              int pitch, uint8_t* __restrict__ q,
                                                              uint8_t* __restrict__ s) {
@@ -110,10 +115,15 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(const T* __restrict
   const long r0 = rb * 128 + (tid >> 4);
   float v[8][8];
   uint32_t a = 0;
+  if (rows - rb * 128 >= 128 && K - c * 128 >= 128) {  // all loads ahead of the first wait
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const long r = r0 + i * 16;
-    load8<T, VEC>(x + r * K + k, r < rows ? min(max(K - k, 0), 8) : 0, v[i]);
+    for (int i = 0; i < 8; ++i) load8<T>(x + (r0 + i * 16) * K + k, 8, v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const long r = r0 + i * 16;
+      load8<T>(x + r * K + k, r < rows ? min(max(K - k, 0), 8) : 0, v[i]);
+    }
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i)
@@ -137,21 +147,13 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(const T* __restrict
 template <typename T>
 hipError_t launch(const T* x, long rows, int K, int block_rows, uint8_t* q, uint8_t* s, hipStream_t st) {
   const int kb = fp8_k_blocks(K), Kp = kb * kFp8Block, pitch = fp8_scale_pitch(K);
-  // whole 16-byte vectors of a row: aligned rows whose length is a multiple of 8
-  const bool vec = ((uintptr_t)x) % 16 == 0 && K % 8 == 0;
   if (block_rows == 1) {
     const int chunks = pitch / 4;
     const dim3 grid = grid_of((rows * chunks + 3) / 4);
-    if (vec)
-      hipLaunchKernelGGL((quantize_rows_kernel<T, true>), grid, dim3(256), 0, st, x, rows, K, Kp, chunks, q, (uint32_t*)s);
-    else
-      hipLaunchKernelGGL((quantize_rows_kernel<T, false>), grid, dim3(256), 0, st, x, rows, K, Kp, chunks, q, (uint32_t*)s);
+    hipLaunchKernelGGL((quantize_rows_kernel<T>), grid, dim3(256), 0, st, x, rows, K, Kp, chunks, q, (uint32_t*)s);
   } else {
     const dim3 grid = grid_of((rows + 127) / 128 * pitch);
-    if (vec)
-      hipLaunchKernelGGL((quantize_tiles_kernel<T, true>), grid, dim3(256), 0, st, x, rows, K, Kp, kb, pitch, q, s);
-    else
-      hipLaunchKernelGGL((quantize_tiles_kernel<T, false>), grid, dim3(256), 0, st, x, rows, K, Kp, kb, pitch, q, s);
+    hipLaunchKernelGGL((quantize_tiles_kernel<T>), grid, dim3(256), 0, st, x, rows, K, Kp, kb, pitch, q, s);
   }
   return hipGetLastError();
 }
