@@ -529,3 +529,23 @@ def test_two_layers_at_once():
         torch.cuda.synchronize()
         for w, ref in zip(sets, alone):
             assert all(torch.equal(w[k], ref[k]) for k in ref)
+
+
+def test_calls_without_a_stream_run_on_the_current_one():
+    torch = _torch()
+    assert dit._stream(None) == torch.cuda.current_stream().cuda_stream
+    side = torch.cuda.Stream()
+    x = torch.randn((5000, 4096), device="cuda", dtype=torch.bfloat16)
+    nc, ns = dit.fp8_layout(5000, 4096, 1)
+    q, s = torch.zeros(nc, dtype=torch.uint8, device="cuda"), torch.zeros(ns, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        assert dit._stream(None) == side.cuda_stream == torch.cuda.current_stream().cuda_stream
+        for _ in range(20):        # each call waits for the copy ahead of it on the same stream alone
+            x.normal_()
+            dit.dit_quantize_fp8(5000, 4096, 1, dit.DIT_BF16, x, q, s)
+        side.synchronize()
+    got = q.clone(), s.clone()
+    dit.dit_quantize_fp8(5000, 4096, 1, dit.DIT_BF16, x, q, s)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], q) and torch.equal(got[1], s)
