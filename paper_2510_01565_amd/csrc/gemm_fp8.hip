@@ -784,8 +784,9 @@ __global__ __launch_bounds__(512) void fp8_rows_kernel(const Fp8Problem p) {
 
 // Which kernel a product takes: the one whose modelled time is least.  In
 // microseconds, rounds of 256 tiles times (a fixed part + a part per K tile of
-// 128), and no less than reading W takes; fitted to 76 shapes (M 1 - 16896, N 33 -
-// 262144, K 64 - 65536; it picks the fastest or one within 13% of it on all of them).
+// 128), of the ring kernels two blocks to a CU and the odd round at a rate of its own,
+// and no less than reading W takes; fitted to 110 shapes (M 1 - 16896, N 33 - 262144,
+// K 64 - 65536; it picks the fastest or one within 15% of it on all of them).
 // Up to 16 rows there is one more, up to a W of 32 MB.  Measured, in us with the
 // launch, bf16 output, these first ones with W not in the caches:
 //   rows         4 x 9216 x 1536 6.1 (16 x 32: 7.1), 16 x 1536 x 6144 8.8 (9.9), but
@@ -794,17 +795,24 @@ __global__ __launch_bounds__(512) void fp8_rows_kernel(const Fp8Problem p) {
 //   32 x 32      128 x 1536 x 6144 7.9 (16 x 32: 9.6, 32 x 64: 9.8)
 //   32 x 64      200 x 1536 x 6144 10.0 (32 x 32: 12.6, 64 x 64: 13.5)
 //   64 x 64      589 x 1536 x 6144 14.8 (32 x 64: 21.5, 128 x 128: 28.5), 589 x 1536 x 1536 6.4
-//   128 x 128    4429 x 1536 x 1536 20.3 (64: 34.3, 256: 25.7), 333 x 6144 x 1536 10.7 (64: 15.6)
-//   256 x 256    4429 x 6144 x 1536 47 (128: 65); a launch of one round leaves the
-//                chip its clock, hence two lines
+//   128 x 128    4429 x 1536 x 1536 17.0 (64: 26.0, 256: 27.0), 333 x 6144 x 1536 10.9 (64: 12.4)
+//   256 x 256    4429 x 6144 x 1536 50 (128: 52.5), 4096^3 63 (128: 73.5); a launch of one
+//                round leaves the chip its clock, hence two lines
 enum Fp8Cfg { FP8_ROWS, FP8_16X32, FP8_32X32, FP8_32X64, FP8_64, FP8_128, FP8_256 };
 static Fp8Cfg pick(int M, int N, int K, int out_dtype) {
   const double kt = fp8_k_blocks(K);
   const bool f32 = out_dtype == DIT_F32;
   if (M <= 16 && N * kt * 128 <= 1 << 25) return FP8_ROWS;
   auto rounds = [&](int bm, int bn) { return ceil(ceil((double)M / bm) * ceil((double)N / bn) / 256.0); };
+  // the ring kernels: c, then a pair of rounds and an odd one, each fixed + per K tile
+  auto ring = [&](int b, double c, double pair, double pair_kt, double odd, double odd_kt) {
+    const double n = rounds(b, b);
+    return c + floor(n / 2) * (pair + pair_kt * kt) + (n - 2 * floor(n / 2)) * (odd + odd_kt * kt);
+  };
   Fp8Cfg cfg = FP8_64;
-  double best = 2.0 + rounds(64, 64) * (1.5 + (f32 ? 0.36 : 0.235) * kt);
+  double best = f32                    ? ring(64, 3.5, 2.45, 0.5, 1.0, 0.31)
+                : rounds(64, 64) <= 1 ? 3.5 + 0.235 * kt
+                                      : ring(64, 2.5, 1.9, 0.385, 0.3, 0.33);
   auto offer = [&](Fp8Cfg c, double us) {
     if (us < best) {
       best = us;
@@ -815,7 +823,9 @@ static Fp8Cfg pick(int M, int N, int K, int out_dtype) {
   offer(FP8_16X32, fmax(2.9 + rounds(16, 32) * (0.7 + (f32 ? 0.065 : 0.06) * kt), memory));
   offer(FP8_32X32, fmax(2.9 + rounds(32, 32) * (1.15 + (f32 ? 0.095 : 0.083) * kt), memory));
   offer(FP8_32X64, fmax(1.7 + rounds(32, 64) * (3.2 + (f32 ? 0.16 : 0.145) * kt), memory));
-  offer(FP8_128, 2.0 + rounds(128, 128) * (2.75 + (f32 ? 1.07 : 0.547) * kt));
+  offer(FP8_128, f32                      ? ring(128, 3.5, 5.7, 1.55, 2.7, 0.92)
+                 : rounds(128, 128) <= 1 ? 4.75 + 0.547 * kt
+                                         : ring(128, 3.1, 3.65, 0.866, 0.0, 0.7));
   // offsets within a tile of 256 output rows fit 32 bits up to 2^21 columns
   if (!f32 && kt >= kMinKTiles256 && N <= 1 << 21)
     offer(FP8_256, rounds(256, 256) <= 1 ? 13.5 + 1.02 * kt : rounds(256, 256) * (7.0 + 1.45 * kt));
@@ -831,11 +841,22 @@ static dim3 ring_grid(long blocks) {
   return dim3((unsigned)std::min(blocks, 1L << kRingRowLog2), (unsigned)((blocks - 1) >> kRingRowLog2) + 1);
 }
 
-template <bool F32, int BM, int BN, int WM, int WN, int KG, int ST>
+// Two stages leave room for a second block on a CU, whose loads and products go on
+// while the first one waits or stores (4429 x 1536 x 1536 17.0 us against 20.5 with
+// four, 11469 x 6574 x 1024 98 against 137, 16896 x 6144 x 1536 fp32 317 against 407).
+// A launch of one block a CU needs four to cover its loads, bf16 ones at any rate (589 x
+// 1536 x 6144 14.9 against 20.0; fp32 20.4 against 21.6, and 18.9 against 19.3 the other way).
+template <bool F32, int BM, int BN, int WM, int WN, int KG>
 static void launch_ring(const Fp8Problem& p, hipStream_t s) {
   const long tiles = (long)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN);
-  const dim3 grid = ring_grid(tiles);
-  hipLaunchKernelGGL((fp8_ring_kernel<F32, BM, BN, WM, WN, KG, ST>), grid, dim3(WM * WN * KG * 64), 0, s, p);
+  const dim3 grid = ring_grid(tiles), block(WM * WN * KG * 64);
+  if constexpr (!F32) {
+    if (tiles <= 256) {
+      hipLaunchKernelGGL((fp8_ring_kernel<F32, BM, BN, WM, WN, KG, 4>), grid, block, 0, s, p);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((fp8_ring_kernel<F32, BM, BN, WM, WN, KG, 2>), grid, block, 0, s, p);
 }
 
 template <bool F32, int FM, int FN>
@@ -851,8 +872,8 @@ static void launch_small(Fp8Cfg cfg, const Fp8Problem& p, hipStream_t s) {
   else if (cfg == FP8_16X32) launch_split<F32, 1, 2>(p, s);
   else if (cfg == FP8_32X32) launch_split<F32, 2, 2>(p, s);
   else if (cfg == FP8_32X64) launch_split<F32, 2, 4>(p, s);
-  else if (cfg == FP8_64) launch_ring<F32, 64, 64, 2, 2, 2, 4>(p, s);
-  else launch_ring<F32, 128, 128, 2, 4, 1, 4>(p, s);
+  else if (cfg == FP8_64) launch_ring<F32, 64, 64, 2, 2, 2>(p, s);
+  else launch_ring<F32, 128, 128, 2, 4, 1>(p, s);
 }
 
 hipError_t launch_gemm_fp8(int M, int N, int K, const void* x, const void* xs, const void* w, const void* ws,

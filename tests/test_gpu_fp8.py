@@ -238,13 +238,14 @@ def _check_large(got, ref, mag, K, out):
 
 
 @pytest.mark.parametrize("M,N,K,bias,off", [
-    (4099, 4111, 257, "bf16", 0),     # 17 x 17 tiles of 256 (one more than the blocks): K tiles 3, odd columns
-    (4099, 4104, 512, "f32", 0),      # 4
-    (4352, 4352, 600, None, 0),       # 5: the scales of the next tile are due one K tile after they are loaded
-    (4097, 4105, 700, "bf16", 1),     # 6, y on an odd element
-    (4100, 8200, 900, "f32", 3),      # 8, two to three tiles a block
+    (8190, 4090, 257, "bf16", 0),     # 32 x 16 tiles of 256, two a block: K tiles 3, ragged edges
+    (8190, 4088, 512, "f32", 0),      # 4
+    (8192, 4096, 600, None, 0),       # 5: the scales of the next tile are due one K tile after they are loaded
+    (8185, 4089, 700, "bf16", 1),     # 6, y on an odd element
+    (8190, 6100, 900, "f32", 3),      # 8, three tiles a block
     (5000, 6001, 1100, "bf16", 0),    # 9
-    (2900, 7100, 1300, None, 5),      # 12 x 28 tiles: some blocks one, some two
+    (7900, 3900, 1300, None, 5),      # 31 x 16 tiles: some blocks one, some two
+    (4090, 4091, 1000, "bf16", 0),    # one tile a block
 ])
 def test_linear_fp8_256x256(M, N, K, bias, off):
     got, ref, mag, ran = _large(M, N, K, "bf16", bias, K, off)
@@ -258,7 +259,8 @@ def test_linear_fp8_256x256(M, N, K, bias, off):
     (70, 1700, 6000, "bf16", "32x32"), (130, 1530, 2000, "f32", "32x32"), (300, 999, 2000, "bf16", "32x64"), (199, 1501, 900, "f32", "32x64"),
     (33, 4001, 300, "bf16", "64x64"), (589, 1536, 6144, "f32", "64x64"), (20, 20000, 700, "bf16", "64x64"),
     (4429, 1530, 1536, "bf16", "128x128"), (4429, 1530, 900, "f32", "128x128"), (4000, 3999, 100, "bf16", "128x128"),
-    (4000, 4001, 257, "f32", "128x128"), (4429, 6144, 1500, "bf16", "256x256"),
+    (4000, 4001, 257, "f32", "128x128"), (1357, 1500, 6000, "bf16", "128x128"), (1101, 1100, 9000, "f32", "64x64"),
+    (1101, 1100, 16000, "bf16", "64x64"), (4429, 6144, 1500, "bf16", "256x256"),
 ])
 def test_linear_fp8_every_kernel(M, N, K, out, cfg):
     """Shapes for which the launch model picks each kernel, on misaligned outputs too (off 1); the profile names it."""
@@ -327,7 +329,7 @@ def _corners(M, N, K, out, seed):
 
 @pytest.mark.parametrize("M,N,K,out,cfg", [
     (66000, 33000, 400, "bf16", "256x256"), (33000, 33001, 130, "f32", "128x128"), (17, 1 << 27, 128, "bf16", "128x128"),
-    (1, (1 << 28) + 5, 128, "bf16", "16x32"),   # more blocks than a row of the grid holds
+    (1, (1 << 28) + 5, 128, "bf16", "128x128"),
 ])
 def test_linear_fp8_offsets_past_32_bits(M, N, K, out, cfg):
     """Outputs of more than 4 GiB, codes of 17 and 34 GB."""
