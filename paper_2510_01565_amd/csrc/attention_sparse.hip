@@ -301,6 +301,8 @@ void launch_select(const double* qm, const double* km, int heads, const SparseMe
 // against 25.9, 4032 x 125 38.2 against 40.2; 8064 x 125 78.1 against 73.6, 3168 x
 // 264 69.0 against 61.1, 12384 x 1032 453 against 302 (means 155 of it).  Past 320
 // key blocks, 516 x 344 28.8 against 33.9 and 1032 x 344 equal: not worth a kernel.
+// Up to 576 key blocks two thread blocks fit a CU, one searching while the other
+// multiplies: 6768 x 563 135 us against 148 with room for 1088 each.
 template <int HD>
 void launch_select(const double* qm, const double* km, int heads, const SparseMeta& m, int text_first, int keep, int* out,
                    hipStream_t s) {
@@ -313,6 +315,8 @@ void launch_select(const double* qm, const double* km, int heads, const SparseMe
   } else if (n <= 320) {
     if (few) launch_select<HD, 5, 4, 8>(qm, km, heads, m, text_first, keep, out, s);
     else launch_select<HD, 5, 16, 4>(qm, km, heads, m, text_first, keep, out, s);
+  } else if (n <= 576) {
+    launch_select<HD, 9, 16, 8>(qm, km, heads, m, text_first, keep, out, s);
   } else if (n <= 1088) {
     launch_select<HD, 17, 16, 16>(qm, km, heads, m, text_first, keep, out, s);
   } else {

@@ -269,6 +269,23 @@ def test_select(reqs, keep, text, dtype, d):
     assert np.array_equal(got, _ref_select(q, k, lens, [r[2] if text else 0 for r in reqs], keep))
 
 
+@pytest.mark.parametrize("reqs,heads,keep,text,dtype,d", [
+    ([(80, 100, 130)], 64, 32, 1, "bf16", 64),                          # 128 key blocks, many rows
+    ([(140, 145, 20)], 1, 50, 1, "f32", 64), ([(140, 145, 20)], 12, 33, 0, "bf16", 64),      # 318, few rows and many
+    ([(150, 150, 7)], 1, 40, 0, "bf16", 128), ([(190, 194, 4)], 2, 576, 1, "bf16", 64), ([(190, 194, 4), (9, 9, 0)], 2, 100, 0, "bf16", 128),
+    ([(200, 200, 0), (12, 12, 70)], 1, 3, 1, "bf16", 128), ([(256, 256, 4096)], 1, 103, 1, "bf16", 64),
+    ([(256, 256, 4097)], 1, 103, 0, "f32", 64),                         # 1089
+])
+def test_select_at_every_length(reqs, heads, keep, text, dtype, d):
+    """Requests at and around the most key blocks that each of the selection's kernels takes."""
+    torch = _torch()
+    b, lens = _batch(reqs)
+    gen = torch.Generator().manual_seed(sum(lens) + heads)
+    q, k = (torch.randn((sum(lens), heads, d), generator=gen).to(_dt(dtype)[0]) for _ in range(2))
+    got = _select(b, heads, d, dtype, q.cuda(), k.cuda(), keep, dit.DIT_SELECT_TEXT if text else 0)
+    assert np.array_equal(got, _ref_select(q, k, lens, [r[2] if text else 0 for r in reqs], keep))
+
+
 @pytest.mark.parametrize("dtype,d", TYPES)
 def test_select_ties_zeros_and_non_finite_scores(dtype, d):
     """Equal scores go to the lower index (all of them, repeated key blocks, both zeros); NaN first; infinities in order."""
