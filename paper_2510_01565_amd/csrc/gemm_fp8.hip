@@ -136,8 +136,10 @@ constexpr int kMinKTiles256 = 3;    // its loads run up to three K tiles ahead, 
 // tile is 4 clusters: cluster c multiplies the wave's c-th quarter of X rows (2
 // fragments) with all its W rows (4 fragments, held for a whole tile, two tiles
 // in turn).  Read phase 4 kt + c takes the X of the next cluster, 4 kt + c + 1, and
-// part c of W of tile kt + 1, whose arrival its next phase waits for.  X's part c
-// of tile kt + 2 and W's of tile kt + 3 are loaded in phase 4 kt + c + 1; loads have
+// part c of W of tile kt + 1; every wave has their data ahead of the first barrier of its
+// next phase, which the other group meets a turn later.  So a place is loaded again two
+// phases after its last read, not one: X's part c of tile kt + 2 in phase 4 kt + c + 1, W's
+// of tile kt + 3 in phase 4 kt + c + 2.  Either is read 6 phases after its load: loads have
 // 5 phases until the wait that makes them visible.
 // A block works through its output tiles as one stream of K tiles: the loads of
 // the next output tile run ahead of the last K tiles of this one, and each
@@ -322,9 +324,10 @@ __global__ __launch_bounds__(512) void fp8_256_kernel(const Fp8Problem p) {
     constexpr int STORE = decltype(storec)::value;
     using CN = std::integral_constant<int, (c + 1) % Q>;
     using SN = std::integral_constant<int, c + 1 < Q ? st : st ^ 1>;  // stage of the next cluster
-    using CP = std::integral_constant<int, (c + Q - 1) % Q>;
+    using CX = std::integral_constant<int, (c + Q - 1) % Q>;
     using SX = std::integral_constant<int, c == 0 ? st ^ 1 : st>;
-    using SW = std::integral_constant<int, c == 0 ? st : st ^ 1>;
+    using CW = std::integral_constant<int, (c + Q - 2) % Q>;
+    using SW = std::integral_constant<int, c < 2 ? st : st ^ 1>;
     if constexpr (STORE == 1) {
       store(cc, prev_m0, prev_n0, bias_stage ^ 1);
 #pragma unroll
@@ -335,8 +338,8 @@ __global__ __launch_bounds__(512) void fp8_256_kernel(const Fp8Problem p) {
           asm volatile("" : "+v"(acc[c * 2 + i][j]));  // zeroed here, ahead of the barrier
         }
     }
-    // the last phase's reads, this cluster's operands among them; complete ahead of the barrier, after which their
-    // places may be loaded again
+    // the last phase's reads, this cluster's operands among them: complete ahead of the barrier, behind which (the next
+    // phase on) their places are loaded again
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
     const int byte = (kt & 3) * 8;
 #pragma unroll
@@ -349,13 +352,11 @@ __global__ __launch_bounds__(512) void fp8_256_kernel(const Fp8Problem p) {
       constexpr int off = (st ^ 1) * STAGE + c * SUB;
       fw[st ^ 1][c] = frag(wa[0] + off, wa[1] + off);
     }
-    // the last part of X's K tile kt + 1 and W's kt + 2, or a part of kt + 2 and kt + 3
-    load_x(SX{}, CP{});
-    load_w(SW{}, CP{});
-    if constexpr (c == 0) {
-      next_xk();
-      next_wk();
-    }
+    // the last part of X's K tile kt + 1, or a part of kt + 2; the last two parts of W's kt + 2, or a part of kt + 3
+    load_x(SX{}, CX{});
+    load_w(SW{}, CW{});
+    if constexpr (c == 0) next_xk();
+    if constexpr (c == 1) next_wk();
     // All but the loads of the last 5 phases have landed.  Those phases' stores need not have: 4 in each phase of the
     // first K tile, if all of the tile's rows and columns exist.
     if (STORE && counted) wait_vmcnt<10 + (STORE == 1 ? 4 * (c + 1) : STORE == 2 ? 16 - 4 * c : 0)>();
@@ -397,9 +398,9 @@ __global__ __launch_bounds__(512) void fp8_256_kernel(const Fp8Problem p) {
   block_barrier();
   static_for<Q - 1>([&](auto cc) {
     load_x(S1{}, cc);
-    load_w(S0{}, cc);
+    if constexpr (decltype(cc)::value > 0) load_w(S0{}, std::integral_constant<int, decltype(cc)::value - 1>{});
   });
-  wait_vmcnt<10>();  // X's first part and the scales among what landed
+  wait_vmcnt<10>();  // what phase 0 reads has landed: X's first two parts, W's first of tile 1 and the scales
   block_barrier();
   read_x(S0{}, S0{}, 0);
   if (wv >= 4) block_barrier();
