@@ -389,8 +389,9 @@ struct SparseArgs {
 // ---------------------------------------------------------------- bf16
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 
-// The running max is raised only when a tile's probabilities against it sum to
-// more than 2^8 in some lane: up to there fp32 and bf16 hold them as well as any.
+// A query's running max is raised only when a tile's probabilities against it sum to
+// more than 2^8 in one of its two lanes: up to there fp32 and bf16 hold them as well as
+// any.  Each query decides for itself, so its bits do not depend on its neighbours.
 constexpr float kLazyMax = 256.0f;
 
 __device__ __forceinline__ void wait_vmcnt0_lgkmcnt0() { __builtin_amdgcn_s_waitcnt(7 << 4); }
@@ -562,15 +563,18 @@ void sparse_bf16_kernel(const SparseArgs a) {
       return t0 + t1;
     };
     float t = probabilities();
-    if (__any(!(t <= kLazyMax))) {
+    const bool high = !(t <= kLazyMax);
+    if (__any(high)) {
+      // a query's two lanes decide alike; the other queries keep their max, and with it their bits
+      const bool raise = (int)high | __shfl_xor((int)high, 32, 64);  // every lane takes part in the exchange
       float tm = s[0][0];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) tm = fmaxf(tm, s[kb][i]);
       tm = fmaxf(mx, fmaxf(tm, __shfl_xor(tm, 32, 64)) * sl2);
-      const float al = __builtin_amdgcn_exp2f(mx - tm);
-      mx = tm;
+      const float al = raise ? __builtin_amdgcn_exp2f(mx - tm) : 1.0f;
+      mx = raise ? tm : mx;
       l *= al;
 #pragma unroll
       for (int db = 0; db < HD / 32; ++db)

@@ -236,6 +236,51 @@ def test_sparse_bits_do_not_depend_on_the_batch(dtype, d):
         row += nq
 
 
+@pytest.mark.parametrize("keep", [5, 10])
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_sparse_bits_do_not_depend_on_the_other_queries(dtype, d, keep):
+    """One query of a block with scores that grow from key block to key block, so that its maximum rises again and again:
+    the bits of every other query of the request stay."""
+    torch = _torch()
+    b, lens = _batch([(16, 40, 0)])     # 640 tokens: 5 query blocks, 10 key blocks
+    heads = 2
+    q, k, v = _qkv(22, 640, heads, d, dtype)
+    k[:, :, 0] = torch.linspace(-1, 1, 640)[:, None].to(k.dtype) * 4   # what the changed query sees
+    q[:, :, 0] = 0
+    blocks = np.broadcast_to(np.arange(keep, dtype=np.int32), (heads, 5, keep)).copy()
+    dev = [x.cuda() for x in (q, k, v)] + [torch.from_numpy(blocks).cuda()]
+    base = _run(b, heads, d, dtype, *dev).clone()
+    _check(base, q, k, v, blocks, lens, dtype)
+    for at in (0, 3, 37, 100, 300):
+        q2 = q.clone()
+        q2[at, :, 0] = 40.0
+        o = _run(b, heads, d, dtype, q2.cuda(), *dev[1:])
+        _check(o, q2, k, v, blocks, lens, dtype)
+        same = [i for i in range(640) if i != at]
+        assert torch.equal(o[same], base[same]), at
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_sparse_bits_do_not_depend_on_the_batch_past_256_query_blocks(dtype, d):
+    """Long lists, every call with more query blocks (times heads) than those whose lists are halved."""
+    torch = _torch()
+    reqs = [(16, 40, 3), (20, 34, 0)]
+    b, lens = _batch(reqs)
+    heads, keep = 64, 11
+    q, k, v = (x.cuda() for x in _qkv(23, sum(lens), heads, d, dtype))
+    blocks = torch.from_numpy(_lists(24, lens, heads, keep)).cuda()
+    packed = _run(b, heads, d, dtype, q, k, v, blocks)
+    off = row = 0
+    for r, L in zip(reqs, lens):
+        nq = -(-L // 128)
+        assert nq * heads > 256
+        alone = _run(_batch([r])[0], heads, d, dtype, *(x[off:off + L].contiguous() for x in (q, k, v)),
+                     blocks[:, row:row + nq].contiguous())
+        assert torch.equal(alone, packed[off:off + L])
+        off += L
+        row += nq
+
+
 # ---------------------------------------------------------------------------- selection
 def _select(b, heads, d, dtype, q, k, keep, flags=0):
     torch = _torch()
