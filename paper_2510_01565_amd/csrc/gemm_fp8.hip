@@ -11,8 +11,10 @@
 // and only at fp32's own limit across them); everything else is summed in fp32.
 // Against 64 bits that is 1.3e-5 (norm) on normal values, a hundredth of the
 // output's own rounding.
-// fp32 output: the codes go through bf16 (exactly, scales included) to the bf16
-// matrix cores, exact products with fp32 sums, at half the rate.
+// fp32 output: the codes go through bf16, exactly, to the bf16 matrix cores, at half
+// the rate: exact products with fp32 sums.  X's codes take both scales with them (a row of
+// X meets one scale of W per K tile), W's none.  All codes at scales of 2^-117 to 2^119 are
+// normal bf16 values; a wave that met others (values near the type's ends) does its sums again.
 #include <math.h>
 
 #include "device_common.h"
@@ -44,12 +46,9 @@ __device__ __forceinline__ float bias_at(const Fp8Problem& p, int n) {
   return p.bias_f32 ? ((const float*)p.bias)[n] : bf2f(((const bf16_t*)p.bias)[n]);
 }
 
-__device__ __forceinline__ float scale_of(uint32_t byte) {
-  return __uint_as_float(byte == 0 ? 0x400000u : byte << 23);  // 2^(byte - 127); 255: +inf, never written
-}
-
-// one lane's 32 codes as bf16 values, 8 to an operand
-__device__ __forceinline__ void to_bf16(const i32x8_t& w, float scale, bf16x8_t* out) {
+// one lane's 32 codes times 2^(byte - 127) as bf16 values, 8 to an operand
+__device__ __forceinline__ void to_bf16(const i32x8_t& w, int byte, bf16x8_t* out) {
+  const float scale = __uint_as_float((uint32_t)byte << 23);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -62,6 +61,9 @@ __device__ __forceinline__ void to_bf16(const i32x8_t& w, float scale, bf16x8_t*
       out[i][4 * j + 3] = b[1];
     }
 }
+// the bytes with which every code, 2^-9 to 448, becomes a normal bf16 value
+constexpr int kLeastByte = 10, kMostByte = 246;
+constexpr uint32_t kBytes = kMostByte - kLeastByte;
 
 // ---------------------------------------------------------------- 256 x 256 tiles, bf16 output
 // s_waitcnt with vmcnt = n and the other counters left alone
@@ -430,18 +432,28 @@ __global__ __launch_bounds__(512) void fp8_256_kernel(const Fp8Problem p) {
 }
 
 // ---------------------------------------------------------------- smaller tiles, and fp32 output
+__device__ __forceinline__ i32x8_t load32(const uint8_t* p, int second) {
+  return __builtin_shufflevector(*(const i32x4_t*)p, *(const i32x4_t*)(p + second), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
 // acc += the products of one K tile's fragments.  bf16 output: the 8-bit cores,
-// scales in the instruction; fp32: codes and scales to bf16, four steps of 32.
+// scales in the instruction; fp32: codes and scales to bf16, four steps of 32.  sx: per
+// row, sw: the same in all of W's fragments; met: more than kBytes once a scale left the range.
 template <bool F32, int FM, int FN>
-__device__ __forceinline__ void multiply(const i32x8_t* x, const i32x8_t* w, const int* sx, const int* sw, f32x4_t (*acc)[FN]) {
+__device__ __forceinline__ void multiply(const i32x8_t* x, const i32x8_t* w, const int* sx, const int* sw, uint32_t& met,
+                                         f32x4_t (*acc)[FN]) {
   if constexpr (F32) {
     bf16x8_t xb[FM][4];
 #pragma unroll
-    for (int i = 0; i < FM; ++i) to_bf16(x[i], scale_of(sx[i] & 255), xb[i]);
+    for (int i = 0; i < FM; ++i) {
+      const uint32_t past = (uint32_t)((sx[i] & 255) + (sw[0] & 255) - 127 - kLeastByte);  // outside the range: more than kBytes
+      met = max(met, past);
+      to_bf16(x[i], (int)past + kLeastByte, xb[i]);
+    }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       bf16x8_t wb[4];
-      to_bf16(w[j], scale_of(sw[j] & 255), wb);
+      to_bf16(w[j], 127, wb);
 #pragma unroll
       for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -453,6 +465,47 @@ __device__ __forceinline__ void multiply(const i32x8_t* x, const i32x8_t* w, con
 #pragma unroll
       for (int j = 0; j < FN; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[j], x[i], acc[i][j], 0, 0, 0, sw[j], 0, sx[i]);
+  }
+}
+
+// The sums of a wave's K tiles kt, kt + step, .. for fp32 output at any scales, straight
+// from memory.  A fragment takes three passes over a K tile where it has rows outside the
+// range: rows within, below and above, the others as zeros.  Below, 2^-117 goes to W, and what
+// is less than 2^-117 even then vanishes in fp32; above, 2^100, and past the range even then
+// every product overflows.  The products are exact wherever the power goes, so a row within
+// gets the bits that multiply() gives it, whatever its neighbours hold.
+// Rows of X from m, of W from n; the lane's codes at byte k of a K tile and `second` further.
+template <int FM, int FN>
+__device__ __forceinline__ void multiply_again(const Fp8Problem& p, int m, int n, int kt, int step, int k, int second,
+                                               f32x4_t (*acc)[FN]) {
+  const int lr = threadIdx.x & 15, Kp = p.kb * kFp8Block;
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (; kt < p.kb; kt += step) {
+    const int sw = p.ws[(long)(n >> 7) * p.pitch + kt];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const long row = min(m + i * 16 + lr, p.M - 1);
+      const i32x8_t x = load32(p.x + row * Kp + kt * 128 + k, second);
+      const int b = p.xs[row * p.pitch + kt] + sw - 127, side = b < kLeastByte ? 1 : b > kMostByte ? 2 : 0;
+#pragma unroll 1
+      for (int pass = 0; pass < 3; ++pass) {
+        if (!__any(side == pass)) continue;
+        const int shift = pass == 0 ? 0 : pass == 1 ? kLeastByte - 127 : 100;
+        bf16x8_t xb[4], wb[4];
+        to_bf16(side == pass ? x : i32x8_t{}, min(max(b - shift, kLeastByte), kMostByte), xb);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          const long col = min(n + (lr >> 2) * (4 * FN) + j * 4 + (lr & 3), p.N - 1);
+          to_bf16(load32(p.w + col * Kp + kt * 128 + k, second), 127 + shift, wb);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[c], xb[c], acc[i][j], 0, 0, 0);
+        }
+      }
+    }
   }
 }
 
@@ -501,7 +554,8 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void fp8_ring_kernel(const Fp8Prob
     return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (long)r0 * pitch), (short)0,
                                              __builtin_amdgcn_readfirstlane(max(min(rows - r0, most), 0) * pitch), kBufferWord3);
   };
-  const int sgo = (wv < BM / 64 ? wv * 64 + lane : lane & 1) * p.pitch;
+  // rows past the last one: its scales
+  const int sgo = (wv < BM / 64 ? min(wv * 64 + lane, p.M - 1 - m0) : lane & 1) * p.pitch;
   auto load = [&](int step, int stage) __attribute__((always_inline)) {
     char* const at = lbase + stage * STAGE;
 #pragma unroll
@@ -536,6 +590,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void fp8_ring_kernel(const Fp8Prob
   }
   const int sxa = SCALES + xr * 4, swa = SCALES + BM * 4 + (((n0 & 127) + wn * FN * 16) >> 7) * 4;
   f32x4_t acc[FM][FN] = {};
+  uint32_t met = 0;
   static_for<ST - 1>([&](auto sc) { load(decltype(sc)::value, decltype(sc)::value); });
   int stage = 0;
   for (int s = 0; s < steps; ++s) {
@@ -558,10 +613,13 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void fp8_ring_kernel(const Fp8Prob
     const int ws = lds4(at + swa) >> byte;  // a wave's columns lie in one row block of scales
 #pragma unroll
     for (int j = 0; j < FN; ++j) sw[j] = ws;
-    multiply<F32, FM, FN>(x, w, sx, sw, acc);
+    multiply<F32, FM, FN>(x, w, sx, sw, met, acc);
     stage = stage + 1 == ST ? 0 : stage + 1;
   }
   wait_vmcnt<0>();
+  if constexpr (F32)
+    if (__any(met > kBytes))
+      multiply_again<FM, FN>(p, m0 + wm * FM * 16, n0 + wn * FN * 16, kg, KG, (lane >> 4) * 16, 64, acc);
   __syncthreads();
   if constexpr (KG > 1) {
     // sums of groups 1 .. at [group - 1][wave of the group][fragment][lane]
@@ -636,8 +694,8 @@ __global__ __launch_bounds__(NW * 64) void fp8_split_kernel(const Fp8Problem p) 
     wo[h] = (uint32_t)((r >> 2) * (4 * FN) + (r & 3)) * (uint32_t)Kp + c;
   }
 #pragma unroll
-  for (int i = 0; i < FM; ++i) so[i] = (i * 16 + lr) * (uint32_t)p.pitch;
-  // rows past the last one read as zeros, and so do K tiles
+  for (int i = 0; i < FM; ++i) so[i] = min(i * 16 + lr, p.M - 1 - m0) * (uint32_t)p.pitch;
+  // rows and K tiles past the last one read as zeros, with the last one's scales
   auto rows = [&](const uint8_t* base, int r0, int most, int n, int pitch) __attribute__((always_inline)) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (long)r0 * pitch), (short)0,
                                              __builtin_amdgcn_readfirstlane(min(n - r0, most) * pitch), kBufferWord3);
@@ -647,8 +705,9 @@ __global__ __launch_bounds__(NW * 64) void fp8_split_kernel(const Fp8Problem p) 
     constexpr int st = decltype(stc)::value;
     const bool in = kt < p.kb;
     const __amdgpu_buffer_rsrc_t rx = rows(p.x, m0, in ? BM : 0, p.M, Kp), rw = rows(p.w, n0, in ? BN : 0, p.N, Kp);
-    const __amdgpu_buffer_rsrc_t rsx = rows(p.xs, m0, in ? BM : 0, p.M, p.pitch);
-    const __amdgpu_buffer_rsrc_t rsw = rows(p.ws, n0 >> 7, in ? 1 : 0, (p.N + 127) >> 7, p.pitch);
+    const __amdgpu_buffer_rsrc_t rsx = rows(p.xs, m0, BM, p.M, p.pitch);
+    const __amdgpu_buffer_rsrc_t rsw = rows(p.ws, n0 >> 7, 1, (p.N + 127) >> 7, p.pitch);
+    const int ks = min(kt, p.kb - 1);
 #pragma unroll
     for (int i = 0; i < BM / 8; ++i) {
       const int vo = (int)xo[i & 1], at = kt * ROWB + i * 8 * Kp;
@@ -662,8 +721,8 @@ __global__ __launch_bounds__(NW * 64) void fp8_split_kernel(const Fp8Problem p) 
           rw, (__attribute__((address_space(3))) void*)(lbase + st * TILE + (BM / 8 + i) * 1024), 16, vo, at, 0, 0);
     }
 #pragma unroll
-    for (int i = 0; i < FM; ++i) sx[st][i] = __builtin_amdgcn_raw_buffer_load_b8(rsx, so[i], kt, 0);
-    sw[st] = __builtin_amdgcn_raw_buffer_load_b8(rsw, 0, kt, 0);
+    for (int i = 0; i < FM; ++i) sx[st][i] = __builtin_amdgcn_raw_buffer_load_b8(rsx, so[i], ks, 0);
+    sw[st] = __builtin_amdgcn_raw_buffer_load_b8(rsw, 0, ks, 0);
     __builtin_amdgcn_sched_barrier(0);
   };
   int fa[2];
@@ -675,6 +734,7 @@ __global__ __launch_bounds__(NW * 64) void fp8_split_kernel(const Fp8Problem p) 
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
   f32x4_t acc[FM][FN] = {};
+  uint32_t met = 0;
   auto step = [&](int kt, auto stc) __attribute__((always_inline)) {
     constexpr int st = decltype(stc)::value;
     wait_vmcnt<LOADS>();  // all but the next K tile's loads
@@ -694,7 +754,7 @@ __global__ __launch_bounds__(NW * 64) void fp8_split_kernel(const Fp8Problem p) 
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): read, before the K tile after the next arrives here
     __builtin_amdgcn_sched_barrier(0);
     load(kt + 2 * NW, stc);
-    multiply<F32, FM, FN>(x, w, xs, ws, acc);
+    multiply<F32, FM, FN>(x, w, xs, ws, met, acc);
     __builtin_amdgcn_sched_barrier(0);
   };
   using S0 = std::integral_constant<int, 0>;
@@ -707,6 +767,8 @@ __global__ __launch_bounds__(NW * 64) void fp8_split_kernel(const Fp8Problem p) 
     step(k + NW, S1{});
   }
   wait_vmcnt<0>();
+  if constexpr (F32)
+    if (__any(met > kBytes)) multiply_again<FM, FN>(p, m0, n0, wv, NW, (lane >> 4) * 16, 64, acc);
   uint4* const sums = lds + lane;
 #pragma unroll
   for (int i = 0; i < FM; ++i)
@@ -729,10 +791,6 @@ __global__ __launch_bounds__(NW * 64) void fp8_split_kernel(const Fp8Problem p) 
 }
 
 // ---------------------------------------------------------------- few rows
-__device__ __forceinline__ i32x8_t load32(const uint8_t* p) {
-  return __builtin_shufflevector(((const i32x4_t*)p)[0], ((const i32x4_t*)p)[1], 0, 1, 2, 3, 4, 5, 6, 7);
-}
-
 // Up to 16 rows of X against 16 columns per block: W is read once, straight from
 // memory to registers, and the block's waves share out the K tiles, two in flight
 // each.  Their sums meet in LDS in wave order.  4 x 9216 x 1536: 6 us with the launch
@@ -748,21 +806,24 @@ __global__ __launch_bounds__(512) void fp8_rows_kernel(const Fp8Problem p) {
   const uint8_t* const x = p.x + (long)min(lr, p.M - 1) * Kp + (lane >> 4) * 32;
   const uint8_t* const xs = p.xs + (long)min(lr, p.M - 1) * p.pitch;
   f32x4_t acc[1][1] = {};
+  uint32_t met = 0;
   for (int k0 = wv; k0 < p.kb; k0 += NW * U) {
     i32x8_t wf[U], xf[U];
     int sw[U], sx[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int kt = min(k0 + u * NW, p.kb - 1);  // past the end: loaded again, not multiplied
-      wf[u] = load32(w + (long)kt * 128);
+      wf[u] = load32(w + (long)kt * 128, 16);
       sw[u] = ws[kt];
-      xf[u] = load32(x + (long)kt * 128);
+      xf[u] = load32(x + (long)kt * 128, 16);
       sx[u] = xs[kt];
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (k0 + u * NW < p.kb) multiply<F32, 1, 1>(&xf[u], &wf[u], &sx[u], &sw[u], acc);
+      if (k0 + u * NW < p.kb) multiply<F32, 1, 1>(&xf[u], &wf[u], &sx[u], &sw[u], met, acc);
   }
+  if constexpr (F32)
+    if (__any(met > kBytes)) multiply_again<1, 1>(p, 0, n0, wv, NW, (lane >> 4) * 32, 16, acc);
   part[wv][lane] = acc[0][0];
   __syncthreads();
   if (wv > 0) return;

@@ -344,3 +344,83 @@ def test_linear_fp8_offsets_past_32_bits(M, N, K, out, cfg):
 def test_linear_fp8_longest_rows(M, N, out, cfg):
     """K of 2^22, the most a row may hold."""
     assert "gemm_fp8_" + cfg in _corners(M, N, 1 << 22, out, 23)[1]
+
+
+@pytest.mark.parametrize("out,M,N,cfg", [
+    ("f32", 3, 40, "rows"), ("f32", 40, 300, "16x32"), ("f32", 250, 900, "32x32"), ("f32", 1100, 1100, "64x64"),
+    ("f32", 4000, 4001, "128x128"), ("bf16", 3, 40, "rows"), ("bf16", 40, 300, "16x32"), ("bf16", 1000, 1000, "64x64"),
+    ("bf16", 4429, 1530, "128x128"), ("bf16", 4090, 4091, "256x256"),
+])
+def test_linear_fp8_the_types_ends(out, M, N, cfg):
+    """Blocks of the largest finite values and of subnormal ones against their opposites, all in the same outputs: x
+    that becomes a code of 256 at 2^120 (as a number, 2^128) and scales of 2^-127 and just above, on either side."""
+    torch = _torch()
+    powers = [128, -121, 0, -120, 119, -119, -127, -118]     # of x's blocks; w's are the opposites
+    K = 128 * len(powers) - 30
+    gen = torch.Generator().manual_seed(M + N)
+    x, w = torch.rand((M, K), generator=gen, dtype=torch.float64) * 2 - 1, torch.randn((N, K), generator=gen, dtype=torch.float64)
+    for j, p in enumerate(powers):
+        x[:, j * 128:(j + 1) * 128] *= 2.0 ** p * (1 - 2.0 ** -24)
+        w[:, j * 128:(j + 1) * 128] *= 2.0 ** (-p - 3)
+    x, w = x.float(), w.float()
+    assert torch.isfinite(x).all() and torch.isfinite(w).all()
+    xq, xs, dxq, dxs = _quantize(x.cuda(), M, K, 1, dit.DIT_F32)
+    wq, ws, dwq, dws = _quantize(w.cuda(), N, K, 128, dit.DIT_F32)
+    assert xs.max() == 247 and xs.min() == 0 and ws.min() <= 1 and (xq[:, :128] == 0x78).any()
+    y = torch.full((M * N + 8,), float("nan"), dtype=_dt(out)[0], device="cuda")
+    dit.profile_start()
+    dit.dit_linear_fp8(M, N, K, dxq, dxs, dwq, dws, None, dit.DIT_F32, y, _dt(out)[1])
+    torch.cuda.synchronize()
+    assert "gemm_fp8_" + cfg in dit.profile_stop()
+    xv, wv = B.dequantize_fp8(xq, xs, 1, K), B.dequantize_fp8(wq, ws, 128, K)
+    ref, mag = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
+    _check(y[:M * N].double().cpu().numpy().reshape(M, N), ref, mag, K, out)
+
+
+@pytest.mark.parametrize("M,N,cfg", [(9, 40, "rows"), (40, 300, "16x32"), (250, 900, "32x32"), (199, 1501, "32x64"),
+                                     (1100, 1100, "64x64"), (4000, 4001, "128x128")])
+def test_linear_fp8_fp32_products_of_any_scales(M, N, cfg):
+    """Scales of both sides together below 2^-117 and above 2^119, where scaled codes no longer fit bf16: rows of either
+    kind beside ordinary ones in every wave, and the ordinary ones' bits as without them."""
+    torch = _torch()
+    rng = np.random.default_rng(M)
+    K, kb = 640 if cfg == "32x64" else 256, 5 if cfg == "32x64" else 2
+    pitch = -(-kb // 4) * 4
+    # K block 0 has w of 2^-17 and large codes, the last one 2^0 to 2^7 and the smallest codes, any others ordinary ones
+    wq = rng.integers(0x30, 0x50, (N, kb * 128))
+    wq[:, :128] = rng.integers(0x50, 0x7f, (N, 128))
+    wq[:, -128:] = rng.integers(1, 9, (N, 128))
+    wq |= rng.integers(0, 2, wq.shape) << 7
+    ws = np.full((-(-N // 128), pitch), 127)
+    ws[:, 0] = 110
+    ws[:, kb - 1] = rng.integers(127, 135, ws.shape[0])
+    plain = rng.integers(0x10, 0x60, (M, kb * 128)) | rng.integers(0, 2, (M, kb * 128)) << 7
+    sx = np.full((M, pitch), 127)
+    sx[:, :kb] = rng.integers(120, 134, (M, kb))
+    xq, xs = plain.copy(), sx.copy()
+    low, high = np.arange(M) % 3 == 0, np.arange(M) % 5 == 1
+    low &= ~high
+    xq[low, :128] = rng.integers(0x50, 0x7f, (low.sum(), 128))          # 16 to 448
+    xq[low, 128:] = 0
+    xs[low, 0] = rng.integers(14, 30, low.sum())                        # with w's 2^-17: 2^-130 to 2^-114
+    xq[high] = rng.integers(1, 9, (high.sum(), kb * 128)) | rng.integers(0, 2, (high.sum(), kb * 128)) << 7   # up to 2^-6
+    xs[high, kb - 1] = rng.integers(240, 248, high.sum())               # with w's 2^7: up to 2^127
+    xs[high, :kb - 1] = rng.integers(200, 248, (high.sum(), kb - 1))
+    together = xs[:, :kb].astype(int)[:, None] + ws[None, :, :kb].astype(int) - 254
+    assert together.min() < -127 and together.max() > 124
+
+    def run(xq, xs):
+        ops = [torch.from_numpy(np.ascontiguousarray(a.astype(np.uint8))).cuda() for a in (xq, xs, wq, ws)]
+        y = torch.full((M * N,), float("nan"), device="cuda")
+        dit.profile_start()
+        dit.dit_linear_fp8(M, N, K, *ops, None, dit.DIT_F32, y, dit.DIT_F32)
+        torch.cuda.synchronize()
+        assert "gemm_fp8_" + cfg in dit.profile_stop()
+        return y.cpu().numpy().reshape(M, N)
+    got, alone = run(xq, xs), run(plain, sx)
+    xv, wv = B.dequantize_fp8(xq, xs, 1, K), B.dequantize_fp8(wq, ws, 128, K)
+    ref, mag = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
+    assert np.abs(ref).max() < 2.0 ** 128 and mag.min() > 2.0 ** -126
+    assert (np.abs(got - ref) <= (K + 2) * 2.0 ** -24 * mag).all(), (np.abs(got - ref) / mag).max()
+    other = ~(low | high)
+    assert other.sum() > 2 and np.array_equal(got[other], alone[other])

@@ -113,7 +113,7 @@ inline void syncthreads() { add(VM, 0, 0); add(LGKM, 0, 0); add(BARRIER, 0, 0); 
 #define __builtin_amdgcn_readfirstlane(x) (x)
 #define __builtin_amdgcn_exp2f exp2f
 #define __builtin_amdgcn_rcpf(x) (1.0f / (x))
-#define __builtin_amdgcn_ldexpf ldexpf
+#define __any(x) (false)
 #define __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, ...) (c)
 #define __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, ...) (c)
 #define __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, ...) bf16x2_t{(__bf16)0.f, (__bf16)0.f}
