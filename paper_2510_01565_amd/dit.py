@@ -122,8 +122,9 @@ def _ptr(x) -> Optional[int]:
 def _stream(s) -> Optional[int]:
     if s is None:
         import torch
-        # the raw handle: 0.3 us, where torch.cuda.current_stream() takes 2.7 to build its object
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        # the raw handle: 0.3 us, where torch.cuda.current_stream() takes 2.7 to build its object, but no public name
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
     if isinstance(s, int):
         return s
     return s.cuda_stream
