@@ -341,7 +341,8 @@ dit_status dit_attention_select(const dit_batch* batch, int heads, int head_dim,
  * a DIT_BF16 call of at most 256 query blocks (times heads) with n_keep >= 8
  * halves every list between two wave groups and adds their sums.  ws: device
  * workspace of at least dit_attention_sparse_workspace_size() bytes, 256-byte
- * aligned; it may be NULL where that size is 0.  o may not overlap k, v or blocks.
+ * aligned; it may be NULL where that size is 0.  o may be q itself; otherwise it may
+ * not overlap q, k, v or blocks.
  */
 dit_status dit_attention_sparse_workspace_size(const dit_batch* batch, int heads, int head_dim, int dtype, size_t* bytes);
 dit_status dit_attention_sparse(const dit_batch* batch, int heads, int head_dim, int dtype, const void* q, const void* k,

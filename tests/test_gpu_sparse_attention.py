@@ -281,6 +281,20 @@ def test_sparse_bits_do_not_depend_on_the_batch_past_256_query_blocks(dtype, d):
         row += nq
 
 
+@pytest.mark.parametrize("keep", [3, 10])
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_sparse_output_over_the_queries(dtype, d, keep):
+    """o may be q itself."""
+    torch = _torch()
+    b, lens = _batch([(20, 33, 7), (1, 5, 0)])
+    q, k, v = (x.cuda() for x in _qkv(25, sum(lens), 3, d, dtype))
+    blocks = torch.from_numpy(_lists(26, lens, 3, keep)).cuda()
+    want = _run(b, 3, d, dtype, q, k, v, blocks)
+    dit.dit_attention_sparse(b, 3, d, _dt(dtype)[1], q, k, v, blocks, keep, q, None, 0)
+    torch.cuda.synchronize()
+    assert torch.equal(q, want)
+
+
 # ---------------------------------------------------------------------------- selection
 def _select(b, heads, d, dtype, q, k, keep, flags=0):
     torch = _torch()
