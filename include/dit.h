@@ -283,7 +283,7 @@ dit_status dit_quantize_fp8(int rows, int K, int block_rows, int dtype, const vo
  * them (the bytes past K are read and must be a code and a scale of finite
  * value in one operand, zeros in the other).  b: N values of type b_dtype, or
  * NULL.  Y is stored as out_dtype.
- *  - DIT_F32: exact products, summed in fp32.
+ *  - DIT_F32: exact products, whatever the scales, summed in fp32.
  *  - DIT_BF16: the 8-bit matrix cores, at twice the rate.  They add each 8
  *    neighbouring products with 14 bits below the largest of them and the rest
  *    in fp32: 1.3e-5 (norm) off on normal values, a hundredth of the output's
@@ -315,9 +315,9 @@ dit_status dit_attention_query_blocks(const dit_batch* batch, int* n_blocks);
 
 /*
  * Chooses the lists: the score of a query block and a key block is the product
- * of the mean query and the mean key, both means and the product in 64 bits,
- * and the n_keep blocks of highest score are kept, the lower index first among
- * equal ones.  A NaN score ranks above every number.  With DIT_SELECT_TEXT in
+ * of the mean query and the mean key, both means and the product in 64 bits
+ * (sums in an order fixed by the tokens' places in their block), and the n_keep
+ * blocks of highest score are kept, the lower index first among equal ones.  A NaN score ranks above every number.  With DIT_SELECT_TEXT in
  * flags the key blocks that hold text rank before all others, in their order.
  * The lists are ascending, with -1 behind the last entry where a request has
  * fewer than n_keep blocks.  q, k as for dit_attention.  ws: device workspace of

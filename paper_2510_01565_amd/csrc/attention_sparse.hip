@@ -3,10 +3,12 @@
 // query block a list names the key blocks it attends to.
 //
 // Selection: the score of (query block i, key block j) is the product of their
-// means.  Means and products are in 64 bits: the answer is a list of indices,
-// which must not depend on the order of a sum, and sums of 64 or 128 bf16 values
-// in 64 bits are exact.  The best n of a row are found by the bits of the n-th
-// largest score, from the highest down.
+// means.  Means and products are in 64 bits: the answer is a list of indices, which
+// roundings of 32 bits would change.  A mean's sum is exact for bf16 blocks whose
+// magnitudes lie within 2^38 of each other; wider ones, fp32 inputs, the division of a
+// shorter last block and the products round, in a fixed order, so that lists repeat, but
+// two blocks of the same tokens in another order may differ in a last place.  The best n
+// of a row are found by the bits of the n-th largest score, from the highest down.
 //
 // Attention: online softmax over the listed blocks, in ascending order.
 #include <float.h>
