@@ -43,8 +43,8 @@ __device__ __forceinline__ long key_mean_at(const SparseMeta& m, int hd, int h, 
 // Block (key or query block, 512 columns of [heads, head_dim]): its mean, 64
 // bits.  A wave reads 1 KB of a token's row at a time and takes every eighth
 // token; the waves' sums meet in LDS.  Every element of Q and K is read once, and
-// that bounds it: 155 us for 66048 tokens of 24 heads of 128, 5.2 TB/s, what a large
-// copy reaches (4.8, reads and writes).
+// that bounds it: 170 us for 66048 tokens of 24 heads of 128, 4.8 TB/s, what a large
+// copy reaches (4.8 - 5.4 by card, reads and writes).
 template <typename T>
 __global__ __launch_bounds__(512) void block_means_kernel(const T* __restrict__ q, const T* __restrict__ k, int heads,
                                                           int hd, const SparseMeta m, double* __restrict__ qm,
@@ -301,7 +301,7 @@ void launch_select(const double* qm, const double* km, int heads, const SparseMe
 // rows of scores exceed LDS.  Both launches of a call in us, 4 against 16 (query
 // blocks times heads x key blocks): 840 x 70 14.4 against 20.4, 1512 x 125 20.5
 // against 25.9, 4032 x 125 38.2 against 40.2; 8064 x 125 78.1 against 73.6, 3168 x
-// 264 69.0 against 61.1, 12384 x 1032 453 against 302 (means 155 of it).  Past 320
+// 264 69.0 against 61.1, 12384 x 1032 453 against 302 (means 170 of it).  Past 320
 // key blocks, 516 x 344 28.8 against 33.9 and 1032 x 344 equal: not worth a kernel.
 // Up to 576 key blocks two thread blocks fit a CU, one searching while the other
 // multiplies: 6768 x 563 135 us against 148 with room for 1088 each.
@@ -418,8 +418,8 @@ __device__ __forceinline__ void read_ahead() {
 // the 4 keys of one dimension), so no copy of V is made and the keys a lane gets
 // are those whose probabilities it holds.
 //
-// 16896 tokens, 24 heads of 128, lists of 33: 450 us, 970 TFLOP/s; three requests of
-// 589 + 1357 + 4429 tokens, 12 heads of 64, lists of 16: 33 us.  The matrix cores are
+// 16896 tokens, 24 heads of 128, lists of 33: 448 - 463 us, 0.95 - 0.98 PFLOP/s; three requests
+// of 589 + 1357 + 4429 tokens, 12 heads of 64, lists of 16: 33.5 us.  The matrix cores are
 // busy half of the time, vector arithmetic (an exponential, a multiply-add, a
 // rounding and a sum per score) for most of the other; neither fewer LDS reads (64
 // queries a wave, head_dim 64: 254 -> 266 us at 16896 tokens) nor a fourth wave per
@@ -675,7 +675,7 @@ void sparse_bf16_kernel(const SparseArgs a) {
 // to registers, in 16-byte pieces: a lane's piece of V holds 4 neighbouring
 // dimensions of a key, each a row of another MFMA.  The next block's K replaces
 // this one's once the scores are done, its V once O is.
-// Measured: 4429 tokens x 24 heads, lists of 18, 375-390 us (82 TF; 498 us with loads
+// Measured: 4429 tokens x 24 heads, lists of 18, 376 - 390 us (82 TF; 498 us with loads
 // where they are used and V in single words), the dense kernel 75 TF; 288 tokens,
 // lists of 2: 6.8 us.  32 queries a block halve the reads and measure the same
 // (379; 589 tokens x 6 heads, lists of 8: 20.4 against 14.2): matrix cores and

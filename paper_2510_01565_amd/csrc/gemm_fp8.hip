@@ -149,7 +149,7 @@ constexpr int kMinKTiles256 = 3;    // its loads run up to three K tiles ahead, 
 // K tile, beside the other group's MFMAs.
 // W's rows are dealt out to the fragments so that a lane holds 16 neighbouring
 // columns of a row: it writes 32 bytes straight from registers.
-// 16896 x 16384 x 4096: 895 - 940 us, 2.4 - 2.5 PFLOP/s, 2.6 - 2.9 at 8192^3 (320 us
+// 16896 x 16384 x 4096: 895 - 960 us, 2.4 - 2.5 PFLOP/s, 2.6 - 2.9 at 8192^3 (320 us
 // without loads, 262 without LDS reads either: matrix cores and clock bound it); the
 // stores, which all CUs issue at the same time, cost about a tenth.  4429 x 6144 x 1536:
 // 47 us, 432 tiles in two rounds of 256.
@@ -905,7 +905,7 @@ static dim3 ring_grid(long blocks) {
 
 // Two stages leave room for a second block on a CU, whose loads and products go on
 // while the first one waits or stores (4429 x 1536 x 1536 17.0 us against 20.5 with
-// four, 11469 x 6574 x 1024 98 against 137, 16896 x 6144 x 1536 fp32 317 against 407).
+// four, 11469 x 6574 x 1024 98 against 137, 16896 x 6144 x 1536 fp32 320 against 407).
 // A launch of one block a CU needs four to cover its loads, bf16 ones at any rate (589 x
 // 1536 x 6144 14.9 against 20.0; fp32 20.4 against 21.6, and 18.9 against 19.3 the other way).
 template <bool F32, int BM, int BN, int WM, int WN, int KG>
