@@ -284,7 +284,7 @@ int main() {
 
 
 def _run(tmp_path, cases, edit=lambda s: s):
-    """The program's lines, one a case; edit: changes the kernels' source first (a checker's own test)."""
+    """The program's lines, one a case; edit: changes the kernels' source first, to see that the check sees it."""
     (tmp_path / "hip").mkdir()
     (tmp_path / "hip" / "hip_runtime.h").write_text(RUNTIME)
     source = edit(open(os.path.join(CSRC, "gemm_fp8.hip")).read())
