@@ -350,6 +350,130 @@ dit_status dit_attention_sparse(const dit_batch* batch, int heads, int head_dim,
                                 void* stream);
 
 /*
+ * 4-bit matrices in the microscaling format: e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4,
+ * 6 and their negatives) with a power-of-two scale per DIT_FP4_BLOCK elements
+ * along K, the same for activations and weights.  For a [rows, K] matrix:
+ *  - codes: two to a byte, the lower nibble first, [rows][128 ceil(K / 256)],
+ *    zeros past column K;
+ *  - scales: one byte each, s = 2^(byte - 127), 255 = NaN, [rows][16 ceil(K / 512)]:
+ *    block 4 i + j of a row's 16 blocks of 512 elements is byte 4 j + i of their
+ *    16 (the order in which the matrix cores take them), 127 past the last block.
+ * dit_fp4_layout returns the bytes of both buffers.  rows >= 0, 1 <= K <= 2^22.
+ */
+#define DIT_FP4_BLOCK 32
+dit_status dit_fp4_layout(int rows, int K, size_t* code_bytes, size_t* scale_bytes);
+
+/*
+ * Quantises x [rows, K] of type dtype.  A block's scale is the smallest power of
+ * two s, at least 2^-127, with |x| <= 6 s for all of the block (1 where it is all
+ * zero); a code is x / s rounded to the nearest e2m1 value, ties to even.  A block
+ * that holds an infinity or a NaN gets the NaN scale and codes of 0: the format has
+ * no other way to say so, and every output that reads the block becomes NaN.
+ * x: any alignment of its elements; codes and scales 16-byte aligned; neither may
+ * overlap x.
+ */
+dit_status dit_quantize_fp4(int rows, int K, int dtype, const void* x, void* codes, void* scales, void* stream);
+
+/*
+ * The values that codes and scales stand for, y [rows, K] of type dtype: exact,
+ * but for those past the type's largest value, which become infinities.  y: any
+ * alignment of its elements; it may overlap neither codes nor scales.
+ */
+dit_status dit_dequantize_fp4(int rows, int K, const void* codes, const void* scales, int dtype, void* y, void* stream);
+
+/*
+ * dit_linear in 4 bits: Y[M, N] = X W^T + b, X [M, K] and W [N, K] as
+ * dit_quantize_fp4 writes them (the bytes past K are read and must be as it writes
+ * them).  b: N values of type b_dtype, or NULL.  Y is stored as out_dtype, rounded
+ * once.  On the 4-bit matrix cores: the sums of a block's products are exact, sums
+ * over blocks are in fp32.  An output's bits depend on its row of X, its row of W,
+ * M and N, not on other rows' values, and are the same on every call.  Codes and
+ * scales 16-byte aligned, b and y aligned to their elements; M, N <= 2^30,
+ * M * N <= 2^36.  y may not overlap the operands.
+ */
+dit_status dit_linear_fp4(int M, int N, int K, const void* x_codes, const void* x_scales, const void* w_codes,
+                          const void* w_scales, const void* b, int b_dtype, void* y, int out_dtype, void* stream);
+
+/*
+ * Rotary positions.  dit_rope_frequencies fills w (host memory, rot_dim / 2
+ * values) with the angle per position of each pair of dimensions,
+ *   w_i = theta^(-2 i / rot_dim) (g_i + (1 - g_i) / factor),
+ * where g_i is 1 for pairs that turn `high` times or more over original_len
+ * positions, 0 for those that turn `low` times or fewer, and linear in the turns
+ * original_len theta^(-2 i / rot_dim) / (2 pi) between: a context extended by
+ * `factor`, whose fast pairs keep their frequencies.  low = high = a number that no
+ * pair reaches divides them all, factor = 1 leaves them all.  2 <= rot_dim <=
+ * DIT_ROPE_MAX_DIM and even, theta > 0, factor >= 1, original_len > 0, 0 <= low <=
+ * high.
+ */
+#define DIT_ROPE_MAX_DIM 256
+dit_status dit_rope_frequencies(int rot_dim, double theta, double factor, double original_len, double low, double high,
+                                double* w);
+
+/*
+ * Turns the first rot_dim dimensions of every head of x [rows][heads][head_dim]
+ * by position times frequency, (a, b) -> magnitude (a cos - b sin, a sin + b cos),
+ * the pairs (a, b) being dimensions i and i + rot_dim / 2 (DIT_ROPE_HALF) or 2 i and
+ * 2 i + 1 (DIT_ROPE_PAIRS); the other dimensions are copied.  ldx, ldy: elements
+ * from one row to the next, at least heads * head_dim, so the query and key heads
+ * of a fused product's rows turn in one call.  positions: int32 device array
+ * [rows], any values; NULL: row r is at position r.  w: host array of rot_dim / 2
+ * frequencies (any finite values), read during the call.  Angles are formed in 64
+ * bits, the rotation in fp32, rounded once to dtype.  y may be x itself with ldy =
+ * ldx; otherwise they may not overlap.  x, y aligned to their elements; rows >= 0,
+ * head_dim <= 1024, rot_dim <= head_dim.
+ */
+#define DIT_ROPE_HALF 0
+#define DIT_ROPE_PAIRS 1
+dit_status dit_rope(int rows, int heads, int head_dim, int rot_dim, int layout, int dtype, const int* positions,
+                    const double* w, float magnitude, const void* x, long ldx, void* y, long ldy, void* stream);
+
+/*
+ * Packed sequences of text.  All arrays are host memory of n_seq entries (1 ..
+ * DIT_MAX_SEQUENCES), read during the call only.  Sequence s has kv_len[s] >= 0
+ * keys and q_len[s] >= 0 queries.  Its queries follow those of the sequences
+ * before it; its keys are the rows kv_row[s], kv_row[s] + 1, .. of k and v (slots
+ * of a cache, or rows that several sequences share), or with kv_row NULL follow the
+ * keys of the sequences before it.
+ */
+#define DIT_MAX_SEQUENCES 128
+typedef struct {
+  int n_seq;
+  const int* q_len;
+  const int* kv_len;
+  const long long* kv_row;
+} dit_sequences;
+
+/*
+ * Attention of packed sequences with grouped heads, O = softmax(scale Q K^T) V:
+ * query head h reads key head h / (heads / kv_heads).  With DIT_CAUSAL in flags the
+ * queries are the last q_len of the kv_len positions (a prompt: q_len = kv_len; one
+ * more token over its cache: q_len = 1), and query i sees the keys 0 .. kv_len -
+ * q_len + i; without it every query sees all keys.  A query that sees no key gets
+ * O = 0.  Keys and values that a query does not see do not reach it, whatever they
+ * hold; rows of k and v outside the sequences are not read.
+ * q [queries][heads][head_dim], k, v [rows][kv_heads][head_dim], o like q, of type
+ * dtype; ldq, ldkv (of k and v), ldo: elements from one row to the next, so the
+ * three may lie in the rows of one fused product.  heads a multiple of kv_heads,
+ * heads <= 1024; head_dim 128 or 64 for DIT_BF16, 64 for DIT_F32; precisions as
+ * for dit_attention; 2^-64 <= scale <= 2^64.  q, k, v, o 16-byte aligned, strides
+ * multiples of 16 bytes and at most 2^22 elements.
+ * ws: device workspace of at least dit_attention_grouped_workspace_size() bytes,
+ * 256-byte aligned, written by every call: calls that may run at once (two
+ * streams, two captured graphs) need one each; it may be NULL where that size is 0.
+ * It holds the partial results of launches with few query tiles, whose keys are cut
+ * into ranges and merged in a fixed order: outputs repeat bit for bit, but their
+ * order of sums follows from the whole batch.  o may be q itself with ldo = ldq;
+ * otherwise it may not overlap q, k or v.
+ */
+#define DIT_CAUSAL 1
+dit_status dit_attention_grouped_workspace_size(const dit_sequences* seqs, int heads, int kv_heads, int head_dim, int dtype,
+                                                size_t* bytes);
+dit_status dit_attention_grouped(const dit_sequences* seqs, int heads, int kv_heads, int head_dim, int dtype, int flags,
+                                 float scale, const void* q, long ldq, const void* k, const void* v, long ldkv, void* o,
+                                 long ldo, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Kernel timing for measurement.  dit_profile_start() makes every later call
  * (from any thread) bracket each kernel launch with a pair of HIP events on
  * the launch's own stream, grouped by kernel family ("gemm_bf16_256x128",

@@ -7,6 +7,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <map>
 #include <mutex>
 #include <string>
@@ -724,6 +725,60 @@ SparseMeta make_sparse_meta(const dit_batch* b) {
   return m;
 }
 
+dit_status check_fp4_shape(int rows, int K) {
+  if (rows < 0 || K <= 0) return fail(DIT_ERR_INVALID_ARG, "rows %d K %d", rows, K);
+  if (K > kFp8MaxK) return fail(DIT_ERR_UNSUPPORTED, "K %d exceeds %d", K, kFp8MaxK);
+  return DIT_OK;
+}
+
+constexpr int kMaxText = 1 << 24;  // queries, or keys of one sequence
+constexpr int kMaxRow = 1 << 22;   // elements between rows: offsets within a tile of 64 keys fit 32 bits
+
+// Checks the sequences and heads, and lays the sequences out longest first: their tiles are numbered in that order,
+// and long ones that start last would end last.
+dit_status check_grouped(const dit_sequences* q, int heads, int kv_heads, int head_dim, int dtype, GroupedArgs* a) {
+  if (!q) return fail(DIT_ERR_INVALID_ARG, "sequences is NULL");
+  if (q->n_seq < 1 || q->n_seq > DIT_MAX_SEQUENCES)
+    return fail(DIT_ERR_INVALID_ARG, "n_seq %d outside [1, %d]", q->n_seq, DIT_MAX_SEQUENCES);
+  if (!q->q_len || !q->kv_len) return fail(DIT_ERR_INVALID_ARG, "q_len / kv_len is NULL");
+  if (dtype != DIT_F32 && dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "dtype %d", dtype);
+  if (heads <= 0 || kv_heads <= 0 || heads % kv_heads != 0)
+    return fail(DIT_ERR_INVALID_ARG, "heads %d kv_heads %d", heads, kv_heads);
+  if (heads > 1024) return fail(DIT_ERR_UNSUPPORTED, "heads %d exceeds 1024", heads);
+  if ((dtype == DIT_BF16 && head_dim != 128 && head_dim != 64) || (dtype == DIT_F32 && head_dim != 64))
+    return fail(DIT_ERR_UNSUPPORTED, "head_dim %d with dtype %d", head_dim, dtype);
+  memset(a, 0, sizeof(*a));
+  a->n_seq = q->n_seq;
+  a->heads = heads;
+  a->kv_heads = kv_heads;
+  a->group = heads / kv_heads;
+  a->head_dim = head_dim;
+  int order[DIT_MAX_SEQUENCES], q_off[DIT_MAX_SEQUENCES];
+  long long kv_off[DIT_MAX_SEQUENCES];
+  long queries = 0;
+  long long keys = 0;
+  for (int s = 0; s < q->n_seq; ++s) {
+    if (q->q_len[s] < 0 || q->kv_len[s] < 0 || (q->kv_row && q->kv_row[s] < 0))
+      return fail(DIT_ERR_INVALID_ARG, "sequence %d: q_len %d kv_len %d", s, q->q_len[s], q->kv_len[s]);
+    if (q->kv_len[s] > kMaxText) return fail(DIT_ERR_UNSUPPORTED, "sequence %d: kv_len %d exceeds %d", s, q->kv_len[s], kMaxText);
+    if (q->kv_row && q->kv_row[s] > 1LL << 40) return fail(DIT_ERR_UNSUPPORTED, "sequence %d: kv_row exceeds 2^40", s);
+    order[s] = s;
+    q_off[s] = (int)queries;
+    kv_off[s] = q->kv_row ? q->kv_row[s] : keys;
+    queries += q->q_len[s];
+    keys += q->kv_len[s];
+    if (queries > kMaxText) return fail(DIT_ERR_UNSUPPORTED, "more than %d queries", kMaxText);
+  }
+  std::stable_sort(order, order + q->n_seq, [&](int x, int y) { return q->kv_len[x] > q->kv_len[y]; });
+  for (int i = 0; i < q->n_seq; ++i) {
+    a->q_off[i] = q_off[order[i]];
+    a->q_len[i] = q->q_len[order[i]];
+    a->kv_len[i] = q->kv_len[order[i]];
+    a->kv_row[i] = kv_off[order[i]];
+  }
+  return DIT_OK;
+}
+
 dit_status check_sparse(const dit_batch* batch, int heads, int head_dim, int dtype, SparseMeta* m) {
   dit_status st;
   if ((st = check_batch(batch, false))) return st;
@@ -1198,6 +1253,172 @@ dit_status dit_attention_sparse(const dit_batch* batch, int heads, int head_dim,
   HIP_TRY(timed(s, "attention_sparse", f, bytes, [&] {
     return launch_attention_sparse(dtype, q, k, v, blocks, n_keep, heads, head_dim, m, o, s);
   }));
+  return DIT_OK;
+}
+
+dit_status dit_fp4_layout(int rows, int K, size_t* code_bytes, size_t* scale_bytes) {
+  g_err.clear();
+  dit_status st;
+  if ((st = check_fp4_shape(rows, K))) return st;
+  if (!code_bytes || !scale_bytes) return fail(DIT_ERR_INVALID_ARG, "code_bytes / scale_bytes is NULL");
+  *code_bytes = (size_t)rows * fp4_pitch(K);
+  *scale_bytes = (size_t)rows * fp4_scale_pitch(K);
+  return DIT_OK;
+}
+
+dit_status dit_quantize_fp4(int rows, int K, int dtype, const void* x, void* codes, void* scales, void* stream) {
+  g_err.clear();
+  dit_status st;
+  if ((st = check_fp4_shape(rows, K))) return st;
+  if (dtype != DIT_F32 && dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "dtype %d", dtype);
+  if (rows == 0) return DIT_OK;
+  if (!x || !codes || !scales) return fail(DIT_ERR_INVALID_ARG, "x / codes / scales is NULL");
+  if (!aligned_to(x, elem_size(dtype))) return fail(DIT_ERR_INVALID_ARG, "x is not aligned to its elements");
+  if (!aligned16(codes) || !aligned16(scales)) return fail(DIT_ERR_INVALID_ARG, "codes and scales must be 16-byte aligned");
+  hipStream_t s = (hipStream_t)stream;
+  const double bytes = (double)rows * ((double)K * elem_size(dtype) + fp4_pitch(K) + fp4_scale_pitch(K));
+  HIP_TRY(timed(s, "quantize_fp4", 0.0, bytes, [&] { return launch_quantize_fp4(dtype, x, rows, K, codes, scales, s); }));
+  return DIT_OK;
+}
+
+dit_status dit_dequantize_fp4(int rows, int K, const void* codes, const void* scales, int dtype, void* y, void* stream) {
+  g_err.clear();
+  dit_status st;
+  if ((st = check_fp4_shape(rows, K))) return st;
+  if (dtype != DIT_F32 && dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "dtype %d", dtype);
+  if (rows == 0) return DIT_OK;
+  if (!codes || !scales || !y) return fail(DIT_ERR_INVALID_ARG, "codes / scales / y is NULL");
+  if (!aligned16(codes) || !aligned16(scales)) return fail(DIT_ERR_INVALID_ARG, "codes and scales must be 16-byte aligned");
+  if (!aligned_to(y, elem_size(dtype))) return fail(DIT_ERR_INVALID_ARG, "y is not aligned to its elements");
+  hipStream_t s = (hipStream_t)stream;
+  const double bytes = (double)rows * ((double)K * elem_size(dtype) + fp4_pitch(K) + fp4_scale_pitch(K));
+  HIP_TRY(timed(s, "dequantize_fp4", 0.0, bytes, [&] { return launch_dequantize_fp4(dtype, codes, scales, rows, K, y, s); }));
+  return DIT_OK;
+}
+
+dit_status dit_linear_fp4(int M, int N, int K, const void* x_codes, const void* x_scales, const void* w_codes,
+                          const void* w_scales, const void* b, int b_dtype, void* y, int out_dtype, void* stream) {
+  g_err.clear();
+  dit_status st;
+  if (N <= 0) return fail(DIT_ERR_INVALID_ARG, "N %d", N);
+  if ((st = check_fp4_shape(M, K))) return st;
+  if (out_dtype != DIT_F32 && out_dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "out_dtype %d", out_dtype);
+  if (b_dtype != DIT_F32 && b_dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "b_dtype %d", b_dtype);
+  if (M > kFp8MaxSide || N > kFp8MaxSide) return fail(DIT_ERR_UNSUPPORTED, "M %d or N %d exceeds 2^30", M, N);
+  if ((double)M * N > kFp8MaxOutputs) return fail(DIT_ERR_UNSUPPORTED, "M %d x N %d exceeds 2^36", M, N);
+  if (M == 0) return DIT_OK;
+  if (!x_codes || !x_scales || !w_codes || !w_scales || !y)
+    return fail(DIT_ERR_INVALID_ARG, "x / w codes or scales or y is NULL");
+  if (!aligned16(x_codes) || !aligned16(w_codes) || !aligned16(x_scales) || !aligned16(w_scales))
+    return fail(DIT_ERR_INVALID_ARG, "codes and scales must be 16-byte aligned");
+  if (!aligned_to(y, elem_size(out_dtype)) || (b && !aligned_to(b, elem_size(b_dtype))))
+    return fail(DIT_ERR_INVALID_ARG, "b / y is not aligned to its elements");
+  hipStream_t s = (hipStream_t)stream;
+  const double bytes = ((double)M + N) * (fp4_pitch(K) + fp4_scale_pitch(K)) + (double)M * N * elem_size(out_dtype);
+  HIP_TRY(timed(s, gemm_fp4_config_name(M, N, K, out_dtype), 2.0 * M * N * (double)K, bytes, [&] {
+    return launch_gemm_fp4(M, N, K, x_codes, x_scales, w_codes, w_scales, b, b_dtype, y, out_dtype, s);
+  }));
+  return DIT_OK;
+}
+
+dit_status dit_rope_frequencies(int rot_dim, double theta, double factor, double original_len, double low, double high,
+                                double* w) {
+  g_err.clear();
+  if (rot_dim < 2 || rot_dim % 2 != 0) return fail(DIT_ERR_INVALID_ARG, "rot_dim %d", rot_dim);
+  if (rot_dim > DIT_ROPE_MAX_DIM) return fail(DIT_ERR_UNSUPPORTED, "rot_dim %d exceeds %d", rot_dim, DIT_ROPE_MAX_DIM);
+  if (!(theta > 0) || !isfinite(theta) || !(factor >= 1) || !isfinite(factor) || !(original_len > 0) || !isfinite(original_len) ||
+      !(low >= 0) || !(high >= low))
+    return fail(DIT_ERR_INVALID_ARG, "theta %g factor %g original_len %g low %g high %g", theta, factor, original_len, low, high);
+  if (!w) return fail(DIT_ERR_INVALID_ARG, "w is NULL");
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    const double f = pow(theta, -2.0 * i / rot_dim), turns = original_len * f / (2 * M_PI);
+    const double g = turns >= high ? 1.0 : turns <= low ? 0.0 : (turns - low) / (high - low);
+    w[i] = f * (g + (1 - g) / factor);
+  }
+  return DIT_OK;
+}
+
+dit_status dit_rope(int rows, int heads, int head_dim, int rot_dim, int layout, int dtype, const int* positions,
+                    const double* w, float magnitude, const void* x, long ldx, void* y, long ldy, void* stream) {
+  g_err.clear();
+  if (rows < 0 || heads <= 0 || head_dim <= 0) return fail(DIT_ERR_INVALID_ARG, "rows %d heads %d head_dim %d", rows, heads, head_dim);
+  if (rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > head_dim) return fail(DIT_ERR_INVALID_ARG, "rot_dim %d of head_dim %d", rot_dim, head_dim);
+  if (rot_dim > DIT_ROPE_MAX_DIM || head_dim > 1024 || heads > 1 << 16)
+    return fail(DIT_ERR_UNSUPPORTED, "rot_dim %d, head_dim %d or heads %d too large", rot_dim, head_dim, heads);
+  if (layout != DIT_ROPE_HALF && layout != DIT_ROPE_PAIRS) return fail(DIT_ERR_INVALID_ARG, "layout %d", layout);
+  if (dtype != DIT_F32 && dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "dtype %d", dtype);
+  if (!w) return fail(DIT_ERR_INVALID_ARG, "w is NULL");
+  for (int i = 0; i < rot_dim / 2; ++i)
+    if (!isfinite(w[i])) return fail(DIT_ERR_INVALID_ARG, "w[%d] is not finite", i);
+  if (!isfinite(magnitude)) return fail(DIT_ERR_INVALID_ARG, "magnitude is not finite");
+  const long width = (long)heads * head_dim;
+  if (ldx < width || ldy < width) return fail(DIT_ERR_INVALID_ARG, "ldx %ld or ldy %ld below heads * head_dim = %ld", ldx, ldy, width);
+  if (rows == 0) return DIT_OK;
+  if (!x || !y) return fail(DIT_ERR_INVALID_ARG, "x / y is NULL");
+  if (!aligned_to(x, elem_size(dtype)) || !aligned_to(y, elem_size(dtype)) || !aligned_to(positions, 4))
+    return fail(DIT_ERR_INVALID_ARG, "x / y / positions is not aligned to its elements");
+  if (x == y && ldx != ldy) return fail(DIT_ERR_INVALID_ARG, "in place with ldx %ld and ldy %ld", ldx, ldy);
+  hipStream_t s = (hipStream_t)stream;
+  const double n = (double)rows * heads * (x == y ? rot_dim : head_dim);
+  HIP_TRY(timed(s, "rope", 0.0, 2.0 * n * elem_size(dtype), [&] {
+    return launch_rope(dtype, rows, heads, head_dim, rot_dim, layout, positions, w, magnitude, x, ldx, y, ldy, s);
+  }));
+  return DIT_OK;
+}
+
+dit_status dit_attention_grouped_workspace_size(const dit_sequences* seqs, int heads, int kv_heads, int head_dim, int dtype,
+                                                size_t* bytes) {
+  g_err.clear();
+  dit_status st;
+  GroupedArgs a;
+  if ((st = check_grouped(seqs, heads, kv_heads, head_dim, dtype, &a))) return st;
+  if (!bytes) return fail(DIT_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = 0;
+  return DIT_OK;
+}
+
+dit_status dit_attention_grouped(const dit_sequences* seqs, int heads, int kv_heads, int head_dim, int dtype, int flags,
+                                 float scale, const void* q, long ldq, const void* k, const void* v, long ldkv, void* o,
+                                 long ldo, void* ws, size_t ws_bytes, void* stream) {
+  g_err.clear();
+  dit_status st;
+  GroupedArgs a;
+  if ((st = check_grouped(seqs, heads, kv_heads, head_dim, dtype, &a))) return st;
+  if (flags & ~DIT_CAUSAL) return fail(DIT_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
+  // positive: the mask's -inf and the running max are of unscaled scores
+  if (!(scale >= 0x1p-64f && scale <= 0x1p64f)) return fail(DIT_ERR_INVALID_ARG, "scale %g outside [2^-64, 2^64]", (double)scale);
+  if (!q || !k || !v || !o) return fail(DIT_ERR_INVALID_ARG, "q / k / v / o is NULL");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o))
+    return fail(DIT_ERR_INVALID_ARG, "q / k / v / o must be 16-byte aligned");
+  const long qw = (long)heads * head_dim, kw = (long)kv_heads * head_dim, per = 16 / elem_size(dtype);
+  if (ldq < qw || ldo < qw || ldkv < kw)
+    return fail(DIT_ERR_INVALID_ARG, "ldq %ld or ldo %ld below %ld, or ldkv %ld below %ld", ldq, ldo, qw, ldkv, kw);
+  if (ldq % per || ldkv % per || ldo % per) return fail(DIT_ERR_INVALID_ARG, "ldq / ldkv / ldo must be multiples of 16 bytes");
+  if (ldq > kMaxRow || ldkv > kMaxRow || ldo > kMaxRow) return fail(DIT_ERR_UNSUPPORTED, "ldq / ldkv / ldo exceeds %d", kMaxRow);
+  if (q == o && ldq != ldo) return fail(DIT_ERR_INVALID_ARG, "in place with ldq %ld and ldo %ld", ldq, ldo);
+  size_t need = 0;
+  dit_attention_grouped_workspace_size(seqs, heads, kv_heads, head_dim, dtype, &need);
+  if (need && (st = check_ws(ws, ws_bytes, need))) return st;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.o = o;
+  a.ldq = ldq;
+  a.ldkv = ldkv;
+  a.ldo = ldo;
+  a.scale = scale;
+  a.causal = flags & DIT_CAUSAL;
+  double pairs = 0, rows = 0, keys = 0;
+  for (int i = 0; i < a.n_seq; ++i) {
+    const double n = a.q_len[i], m = a.kv_len[i], below = fmax(n - m, 0.0);  // queries that see nothing
+    pairs += a.causal ? (n - below) * (2 * m - (n - below) + 1) / 2 : n * m;
+    rows += n;
+    keys += m;
+  }
+  hipStream_t s = (hipStream_t)stream;
+  const double bytes = 2.0 * (rows * heads + keys * kv_heads) * head_dim * elem_size(dtype);
+  HIP_TRY(timed(s, "attention_grouped", 4.0 * pairs * heads * head_dim, bytes,
+                [&] { return launch_attention_grouped(dtype, a, s); }));
   return DIT_OK;
 }
 

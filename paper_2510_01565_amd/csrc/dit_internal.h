@@ -298,4 +298,38 @@ hipError_t launch_attention_select(int dtype, const void* q, const void* k, int 
 hipError_t launch_attention_sparse(int dtype, const void* q, const void* k, const void* v, const int* blocks, int keep,
                                    int heads, int head_dim, const SparseMeta& m, void* o, hipStream_t s);
 
+// ----------------------------------------------------------------------------
+// 4-bit matrices: bytes of a row of codes (zeros past K) and of scales
+inline int fp4_pitch(int K) { return (K + 255) / 256 * 128; }
+inline int fp4_scale_pitch(int K) { return (K + 511) / 512 * 16; }
+
+hipError_t launch_quantize_fp4(int dtype, const void* x, long rows, int K, void* q, void* scales, hipStream_t s);
+hipError_t launch_dequantize_fp4(int dtype, const void* q, const void* scales, long rows, int K, void* y, hipStream_t s);
+hipError_t launch_gemm_fp4(int M, int N, int K, const void* x, const void* xs, const void* w, const void* ws,
+                           const void* bias, int bias_dtype, void* y, int out_dtype, hipStream_t s);
+// name of the kernel launch_gemm_fp4 picks
+const char* gemm_fp4_config_name(int M, int N, int K, int out_dtype);
+
+// rotary positions; w: host array of rot / 2 angles per position
+hipError_t launch_rope(int dtype, long rows, int heads, int d, int rot, int layout, const int* pos, const double* w,
+                       float magnitude, const void* x, long ldx, void* y, long ldy, hipStream_t s);
+
+// ----------------------------------------------------------------------------
+// Attention of packed sequences with grouped heads.  The `group` = heads / kv_heads query heads that share a key head are
+// rows of the same tiles: row i * group + g of a sequence is its query i at head kv_head * group + g.
+struct GroupedArgs {
+  const void *q, *k, *v;
+  void* o;
+  long ldq, ldkv, ldo;
+  int n_seq, heads, kv_heads, group, head_dim, causal;
+  float scale;
+  // sequences in the order in which their tiles are numbered, longest first
+  int q_off[DIT_MAX_SEQUENCES];    // first query
+  int q_len[DIT_MAX_SEQUENCES];
+  int kv_len[DIT_MAX_SEQUENCES];
+  long kv_row[DIT_MAX_SEQUENCES];  // first row of k and v
+  int tile_off[DIT_MAX_SEQUENCES + 1];  // row tiles of the sequences before
+};
+hipError_t launch_attention_grouped(int dtype, const GroupedArgs& a, hipStream_t s);
+
 }  // namespace dit

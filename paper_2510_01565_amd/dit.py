@@ -25,12 +25,19 @@ DIT_NOALLOC_SCRATCH_BYTES = 256 << 20
 DIT_FP8_BLOCK = 128
 DIT_SPARSE_QUERIES, DIT_SPARSE_KEYS, DIT_SPARSE_MAX_KEY_BLOCKS = 128, 64, 2048
 DIT_SELECT_TEXT = 1
+DIT_FP4_BLOCK = 32
+DIT_ROPE_MAX_DIM = 256
+DIT_ROPE_HALF, DIT_ROPE_PAIRS = 0, 1
+DIT_MAX_SEQUENCES = 128
+DIT_CAUSAL = 1
 
 EXPORTED = ("dit_weight_count", "dit_weight_manifest", "dit_workspace_size", "dit_step", "dit_step_noalloc",
             "dit_block_forward", "euler_update", "dit_attention_workspace_size", "dit_attention", "dit_linear",
             "dit_fp8_layout", "dit_quantize_fp8", "dit_linear_fp8", "dit_attention_query_blocks",
             "dit_attention_select_workspace_size", "dit_attention_select", "dit_attention_sparse_workspace_size",
-            "dit_attention_sparse", "dit_profile_start", "dit_profile_stop", "dit_profile_entry", "dit_last_error")
+            "dit_attention_sparse", "dit_fp4_layout", "dit_quantize_fp4", "dit_dequantize_fp4", "dit_linear_fp4",
+            "dit_rope_frequencies", "dit_rope", "dit_attention_grouped_workspace_size", "dit_attention_grouped",
+            "dit_profile_start", "dit_profile_stop", "dit_profile_entry", "dit_last_error")
 
 
 class DitError(RuntimeError):
@@ -51,6 +58,11 @@ class dit_batch(ctypes.Structure):
     _fields_ = [("n_req", ctypes.c_int), ("grid_h", ctypes.POINTER(ctypes.c_int)),
                 ("grid_w", ctypes.POINTER(ctypes.c_int)), ("n_txt", ctypes.POINTER(ctypes.c_int)),
                 ("t", ctypes.POINTER(ctypes.c_float))]
+
+
+class dit_sequences(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int), ("q_len", ctypes.POINTER(ctypes.c_int)), ("kv_len", ctypes.POINTER(ctypes.c_int)),
+                ("kv_row", ctypes.POINTER(ctypes.c_longlong))]
 
 
 class dit_weights(ctypes.Structure):
@@ -94,6 +106,15 @@ def lib() -> ctypes.CDLL:
         L.dit_attention_select.argtypes = [bp, ip, ip, ip, vp, vp, ip, ip, vp, vp, sz, vp]
         L.dit_attention_sparse_workspace_size.argtypes = [bp, ip, ip, ip, sp]
         L.dit_attention_sparse.argtypes = [bp, ip, ip, ip, vp, vp, vp, vp, ip, vp, vp, sz, vp]
+        dbl, lng, flt, qp = ctypes.c_double, ctypes.c_long, ctypes.c_float, ctypes.POINTER(dit_sequences)
+        L.dit_fp4_layout.argtypes = [ip, ip, sp, sp]
+        L.dit_quantize_fp4.argtypes = [ip, ip, ip, vp, vp, vp, vp]
+        L.dit_dequantize_fp4.argtypes = [ip, ip, vp, vp, ip, vp, vp]
+        L.dit_linear_fp4.argtypes = [ip, ip, ip, vp, vp, vp, vp, vp, ip, vp, ip, vp]
+        L.dit_rope_frequencies.argtypes = [ip, dbl, dbl, dbl, dbl, dbl, ctypes.POINTER(dbl)]
+        L.dit_rope.argtypes = [ip, ip, ip, ip, ip, ip, vp, ctypes.POINTER(dbl), flt, vp, lng, vp, lng, vp]
+        L.dit_attention_grouped_workspace_size.argtypes = [qp, ip, ip, ip, ip, sp]
+        L.dit_attention_grouped.argtypes = [qp, ip, ip, ip, ip, ip, flt, vp, lng, vp, vp, lng, vp, lng, vp, sz, vp]
         L.dit_profile_start.argtypes = []
         L.dit_profile_stop.argtypes = [ctypes.POINTER(ctypes.c_int)]
         L.dit_profile_entry.argtypes = [ip, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(ctypes.c_long),
@@ -271,6 +292,73 @@ def dit_attention_sparse(batch: Batch, heads: int, head_dim: int, dtype: int, q,
                          ws_bytes: int, stream=None) -> None:
     _check(lib().dit_attention_sparse(ctypes.byref(batch.c), heads, head_dim, dtype, _ptr(q), _ptr(k), _ptr(v),
                                       _ptr(blocks), n_keep, _ptr(o), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def fp4_layout(rows: int, K: int) -> Tuple[int, int]:
+    """Bytes of the codes and of the scales of a [rows, K] 4-bit matrix."""
+    c, s = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(lib().dit_fp4_layout(rows, K, ctypes.byref(c), ctypes.byref(s)))
+    return c.value, s.value
+
+
+def dit_quantize_fp4(rows: int, K: int, dtype: int, x, codes, scales, stream=None) -> None:
+    _check(lib().dit_quantize_fp4(rows, K, dtype, _ptr(x), _ptr(codes), _ptr(scales), _stream(stream)))
+
+
+def dit_dequantize_fp4(rows: int, K: int, codes, scales, dtype: int, y, stream=None) -> None:
+    _check(lib().dit_dequantize_fp4(rows, K, _ptr(codes), _ptr(scales), dtype, _ptr(y), _stream(stream)))
+
+
+def dit_linear_fp4(M: int, N: int, K: int, x_codes, x_scales, w_codes, w_scales, b, b_dtype: int, y, out_dtype: int,
+                   stream=None) -> None:
+    _check(lib().dit_linear_fp4(M, N, K, _ptr(x_codes), _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), _ptr(b), b_dtype,
+                                _ptr(y), out_dtype, _stream(stream)))
+
+
+def rope_frequencies(rot_dim: int, theta: float, factor: float = 1.0, original_len: float = 1.0, low: float = 0.0,
+                     high: float = 0.0):
+    """Host array of rot_dim / 2 angles per position (doubles), for ``dit_rope``."""
+    w = (ctypes.c_double * max(rot_dim // 2, 1))()
+    _check(lib().dit_rope_frequencies(rot_dim, theta, factor, original_len, low, high, w))
+    return w
+
+
+def dit_rope(rows: int, heads: int, head_dim: int, rot_dim: int, layout: int, dtype: int, positions, w, magnitude: float, x,
+             ldx: int, y, ldy: int, stream=None) -> None:
+    """``w``: what ``rope_frequencies`` returns, or a sequence of rot_dim / 2 numbers."""
+    if w is not None and not isinstance(w, ctypes.Array):
+        w = (ctypes.c_double * len(w))(*w)
+    if w is not None and 2 * len(w) < rot_dim:
+        raise ValueError(f"{len(w)} frequencies for {rot_dim} dimensions")
+    _check(lib().dit_rope(rows, heads, head_dim, rot_dim, layout, dtype, _ptr(positions), w, magnitude, _ptr(x), ldx, _ptr(y),
+                          ldy, _stream(stream)))
+
+
+class Sequences:
+    """Owns the host arrays of a dit_sequences."""
+
+    def __init__(self, q_len: Sequence[int], kv_len: Sequence[int], kv_row: Optional[Sequence[int]] = None):
+        n = len(q_len)
+        if len(kv_len) != n or (kv_row is not None and len(kv_row) != n):
+            raise ValueError("q_len, kv_len and kv_row must have one entry per sequence")
+        self.n = n
+        self._q = (ctypes.c_int * n)(*q_len)
+        self._kv = (ctypes.c_int * n)(*kv_len)
+        self._row = (ctypes.c_longlong * n)(*kv_row) if kv_row is not None else None
+        self.c = dit_sequences(n, self._q, self._kv,
+                               ctypes.cast(self._row, ctypes.POINTER(ctypes.c_longlong)) if self._row is not None else None)
+
+
+def attention_grouped_workspace_size(seqs: Sequences, heads: int, kv_heads: int, head_dim: int, dtype: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().dit_attention_grouped_workspace_size(ctypes.byref(seqs.c), heads, kv_heads, head_dim, dtype, ctypes.byref(n)))
+    return n.value
+
+
+def dit_attention_grouped(seqs: Sequences, heads: int, kv_heads: int, head_dim: int, dtype: int, flags: int, scale: float, q,
+                          ldq: int, k, v, ldkv: int, o, ldo: int, ws, ws_bytes: int, stream=None) -> None:
+    _check(lib().dit_attention_grouped(ctypes.byref(seqs.c), heads, kv_heads, head_dim, dtype, flags, scale, _ptr(q), ldq,
+                                       _ptr(k), _ptr(v), ldkv, _ptr(o), ldo, _ptr(ws), ws_bytes, _stream(stream)))
 
 
 def profile_start() -> None:
