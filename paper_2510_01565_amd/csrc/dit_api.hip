@@ -1373,7 +1373,7 @@ dit_status dit_attention_grouped_workspace_size(const dit_sequences* seqs, int h
   GroupedArgs a;
   if ((st = check_grouped(seqs, heads, kv_heads, head_dim, dtype, &a))) return st;
   if (!bytes) return fail(DIT_ERR_INVALID_ARG, "bytes is NULL");
-  *bytes = 0;
+  *bytes = align256(attention_grouped_bytes(dtype, a));
   return DIT_OK;
 }
 
@@ -1396,8 +1396,7 @@ dit_status dit_attention_grouped(const dit_sequences* seqs, int heads, int kv_he
   if (ldq % per || ldkv % per || ldo % per) return fail(DIT_ERR_INVALID_ARG, "ldq / ldkv / ldo must be multiples of 16 bytes");
   if (ldq > kMaxRow || ldkv > kMaxRow || ldo > kMaxRow) return fail(DIT_ERR_UNSUPPORTED, "ldq / ldkv / ldo exceeds %d", kMaxRow);
   if (q == o && ldq != ldo) return fail(DIT_ERR_INVALID_ARG, "in place with ldq %ld and ldo %ld", ldq, ldo);
-  size_t need = 0;
-  dit_attention_grouped_workspace_size(seqs, heads, kv_heads, head_dim, dtype, &need);
+  const size_t need = align256(attention_grouped_bytes(dtype, a));
   if (need && (st = check_ws(ws, ws_bytes, need))) return st;
   a.q = q;
   a.k = k;
@@ -1408,6 +1407,7 @@ dit_status dit_attention_grouped(const dit_sequences* seqs, int heads, int kv_he
   a.ldo = ldo;
   a.scale = scale;
   a.causal = flags & DIT_CAUSAL;
+  a.part = (float*)ws;
   double pairs = 0, rows = 0, keys = 0;
   for (int i = 0; i < a.n_seq; ++i) {
     const double n = a.q_len[i], m = a.kv_len[i], below = fmax(n - m, 0.0);  // queries that see nothing

@@ -328,8 +328,14 @@ struct GroupedArgs {
   int q_len[DIT_MAX_SEQUENCES];
   int kv_len[DIT_MAX_SEQUENCES];
   long kv_row[DIT_MAX_SEQUENCES];  // first row of k and v
-  int tile_off[DIT_MAX_SEQUENCES + 1];  // row tiles of the sequences before
+  // Set by the launcher.  Row tiles of the sequences before, a tile's key ranges counted one by one; a sequence of more than
+  // `chunk` keys is cut into ranges of `chunk`, whose partial results go to `part` and are merged by a second kernel.
+  int tile_off[DIT_MAX_SEQUENCES + 1];
+  int chunk;
+  float* part;
 };
+// bytes of `part` that any launch of these sequences needs, causal or not
+size_t attention_grouped_bytes(int dtype, const GroupedArgs& a);
 hipError_t launch_attention_grouped(int dtype, const GroupedArgs& a, hipStream_t s);
 
 }  // namespace dit
