@@ -73,24 +73,27 @@ __device__ __forceinline__ int seen_by(const GroupedArgs& a, int s, int i) {
 
 struct Unit {
   int s, h, row0, rows;     // sequence, key head, first row of the tile, rows of the sequence
-  int begin, end, ranges;   // its range of the keys, and how many ranges there are
+  int begin, end, ranges;   // its range of the keys, and how many ranges the tile has
 };
-// key ranges of sequence s
+// key ranges that a sequence's tiles may have; a tile that sees fewer keys has fewer
 __host__ __device__ __forceinline__ int ranges_of(const GroupedArgs& a, int s) {
   return a.kv_len[s] > a.chunk ? (a.kv_len[s] + a.chunk - 1) / a.chunk : 1;
 }
-// Unit `id` of tiles of `per` rows: key heads in turn, then the ranges of a tile; a sequence's last tile, which sees most, first.
+// Unit `id` of tiles of `per` rows: key heads in turn, then the ranges of a tile; a sequence's last tile, which sees most,
+// first.  The ranges of a tile are equal but for whole key tiles.  begin > end: a range that the tile does not have.
 __device__ __forceinline__ Unit unit_of(const GroupedArgs& a, int id, int per) {
   Unit u;
   const int t = id / a.kv_heads;
   u.h = id - t * a.kv_heads;
   u.s = sequence_of(a, t);
   u.rows = a.q_len[u.s] * a.group;
-  u.ranges = ranges_of(a, u.s);
-  const int n = a.tile_off[u.s + 1] - 1 - t, tile = n / u.ranges, range = u.ranges - 1 - (n - tile * u.ranges);
+  const int most = ranges_of(a, u.s), n = a.tile_off[u.s + 1] - 1 - t, tile = n / most, range = most - 1 - (n - tile * most);
   u.row0 = tile * per;
-  u.begin = range * a.chunk;
-  u.end = u.ranges > 1 ? min(u.begin + a.chunk, a.kv_len[u.s]) : a.kv_len[u.s];
+  const int seen = seen_by(a, u.s, (min(u.row0 + per, u.rows) - 1) / a.group);
+  u.ranges = seen > a.chunk ? (seen + a.chunk - 1) / a.chunk : 1;
+  const int len = ((seen + u.ranges - 1) / u.ranges + kKeys - 1) / kKeys * kKeys;
+  u.begin = range * len;
+  u.end = range < u.ranges ? min(u.begin + len, seen) : -1;
   return u;
 }
 // where a unit's partial results lie: O [rows of a tile][HD], unnormalised; behind all of them (max, sum) [rows of a tile]
@@ -125,9 +128,10 @@ void grouped_bf16_kernel(const GroupedArgs a) {
   const bf16_t* const K = (const bf16_t*)a.k + a.kv_row[u.s] * a.ldkv + (long)u.h * HD;
   const bf16_t* const V = (const bf16_t*)a.v + a.kv_row[u.s] * a.ldkv + (long)u.h * HD;
   const int last = u.rows - 1;
+  if (u.end < 0) return;
   // key tiles from the range's first on: all, and those that every row sees
   const int first = u.begin / kKeys;
-  const int tiles = (min(seen_by(a, u.s, min(u.row0 + ROWS - 1, last) / G), u.end) + kKeys - 1) / kKeys;
+  const int tiles = (u.end + kKeys - 1) / kKeys;
   const int whole = min(seen_by(a, u.s, u.row0 / G), u.end) / kKeys;
   const int wave_seen = seen_by(a, u.s, min(u.row0 + wave * 32 + 31, last) / G);     // keys that some row of this wave sees
 
@@ -311,7 +315,7 @@ void grouped_bf16_kernel(const GroupedArgs a) {
                                   __uint_as_float(v.y & 0xffff0000)};
 #pragma unroll
               for (int r = 0; r < 4; ++r)
-                if (in && !is_finite(f[r])) o[db][q * 4 + r] = fmaf(pr, f[r], o[db][q * 4 + r]);
+                o[db][q * 4 + r] = fmaf(pr, in && !is_finite(f[r]) ? f[r] : 0.f, o[db][q * 4 + r]);
               __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -380,8 +384,9 @@ __global__ __launch_bounds__(256) void grouped_f32_kernel(const GroupedArgs a) {
   const int L = a.kv_len[u.s], G = a.group, last = u.rows - 1;
   const float* const K = (const float*)a.k + a.kv_row[u.s] * a.ldkv + (long)u.h * FD;
   const float* const V = (const float*)a.v + a.kv_row[u.s] * a.ldkv + (long)u.h * FD;
+  if (u.end < 0) return;
   const int first = u.begin / kKeys;
-  const int tiles = (min(seen_by(a, u.s, min(u.row0 + FQ - 1, last) / G), u.end) + kKeys - 1) / kKeys;
+  const int tiles = (u.end + kKeys - 1) / kKeys;
   const int least = seen_by(a, u.s, u.row0 / G);  // keys that every row sees
   const int row = min(u.row0 + lr, last), query = row / G;
   const int seen = seen_by(a, u.s, query);
@@ -519,10 +524,13 @@ __global__ __launch_bounds__(256) void grouped_f32_kernel(const GroupedArgs a) {
 
 // ---------------------------------------------------------------- bf16, few rows
 // Sequences of at most 32 rows: one token, or a few, over a cache.  A block takes a
-// range of the keys; its two waves take tiles of 32 keys in turn, each for all rows,
-// with stages of LDS, a running max, a sum and an O of its own: no barrier until they
-// meet at the end.  The reads of K and V bound it.
-constexpr int kFewRows = 32, kFewKeys = 32;
+// range of the keys; its four waves take tiles of 32 keys in turn, each for all rows,
+// with LDS, a running max, a sum and an O of its own: no barrier until they meet at the
+// end.  A tile's K goes to registers whole, and the next tile's K into its place while
+// the softmax runs; its V likewise, the next one's arriving beside the next scores.  So
+// one place each is enough, two blocks share a CU, and what a CU has in flight is what
+// its LDS holds.  The reads of K and V bound it.
+constexpr int kFewRows = 32, kFewKeys = 32, kFewWaves = 4;
 
 __device__ __forceinline__ void wait_lgkmcnt0() { __builtin_amdgcn_s_waitcnt(0xc07f); }
 template <int n>
@@ -532,63 +540,54 @@ __device__ __forceinline__ void wait_vmcnt() {
 }
 
 template <int HD>
-__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(kFewWaves * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void grouped_few_kernel(const GroupedArgs a) {
-  constexpr int NW = 2;
+  constexpr int NW = kFewWaves;
   constexpr int CH = HD / 8, RPI = 64 / CH, NI = kFewKeys / RPI;  // chunks of a row, rows and number of loads of a tile
-  constexpr int ROWB = HD * 2, TILE = kFewKeys * ROWB, STAGE = 2 * TILE;
-  __shared__ uint4 smem[NW * 2 * STAGE / 16];  // [wave][stage][K tile | V tile], then the second wave's results
+  constexpr int ROWB = HD * 2, TILE = kFewKeys * ROWB;
+  constexpr int NR = HD / 2, MERGE = NW * (NR + 2) * 64 * 4;  // registers of O, bytes of all waves' results
+  // [wave][K tile | V tile], then [wave][register][lane] of the results
+  __shared__ uint4 smem[(MERGE > NW * 2 * TILE ? MERGE : NW * 2 * TILE) / 16];
   const int id = block_id();
   if (id >= a.tile_off[a.n_seq] * a.kv_heads) return;
   const Unit u = unit_of(a, id, kFewRows);
+  if (u.end < 0) return;
   const int tid = threadIdx.x, lane = tid & 63, hl = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  char* const lbase = (char*)smem + wave * 2 * STAGE;
-  const int G = a.group, ld = (int)a.ldkv, last = u.rows - 1;
+  char* const lbase = (char*)smem + wave * 2 * TILE;
+  const int G = a.group, ld = (int)a.ldkv, last = u.rows - 1, end = u.end;
   const bf16_t* const K = (const bf16_t*)a.k + a.kv_row[u.s] * a.ldkv + (long)u.h * HD;
   const bf16_t* const V = (const bf16_t*)a.v + a.kv_row[u.s] * a.ldkv + (long)u.h * HD;
-  const int end = min(seen_by(a, u.s, last / G), u.end);  // of the range's keys that some row sees
-  const int least = seen_by(a, u.s, 0);                   // keys that every row sees
+  const int least = min(seen_by(a, u.s, 0), end);  // keys that every row sees
 
   auto kswz = [](int key, int c) { return HD == 128 ? c ^ (key & 15) : c ^ ((key >> 1) & 7); };
   auto vswz = [](int key, int c) { return HD == 128 ? c ^ ((key & 3) << 2) : c ^ ((key & 2) << 1); };
-  int ko[NI], vo[NI];
-#pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int key = i * RPI + lane / CH;
-    ko[i] = (key * ld + kswz(key, lane % CH) * 8) * 2;
-    vo[i] = (key * ld + vswz(key, lane % CH) * 8) * 2;
-  }
-  // keys k0 .. of a tile into stage st; keys past the range read as zeros, a tile past it touches no memory
-  auto tile_load = [&](int k0, int st) __attribute__((always_inline)) {
+  // keys k0 .. of a tile; keys past the range read as zeros, a tile past it touches no memory
+  auto load = [&](const bf16_t* base, int k0, bool value) __attribute__((always_inline)) {
     const int n = min(end - k0, kFewKeys), bytes = __builtin_amdgcn_readfirstlane(n > 0 ? ((n - 1) * ld + HD) * 2 : 0);
-    const long off = (long)(n > 0 ? k0 : 0) * ld;
-    const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(K + off), (short)0, bytes, kBufferWord3);
-    const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(V + off), (short)0, bytes, kBufferWord3);
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(base + (long)(n > 0 ? k0 : 0) * ld), (short)0, bytes, kBufferWord3);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const int o = ko[i];
+      const int key = i * RPI + lane / CH, c = value ? vswz(key, lane % CH) : kswz(key, lane % CH);
+      const int o = (key * ld + c * 8) * 2;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rk, (__attribute__((address_space(3))) void*)(lbase + st * STAGE + i * 1024), 16, o, 0, 0, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int o = vo[i];
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rv, (__attribute__((address_space(3))) void*)(lbase + st * STAGE + TILE + i * 1024), 16, o, 0, 0, 0);
+          r, (__attribute__((address_space(3))) void*)(lbase + (value ? TILE : 0) + i * 1024), 16, o, 0, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
   const int row = lane & 31, query = min(row, last) / G, head = u.h * G + min(row, last) - query * G;
-  const int seen = seen_by(a, u.s, query);
+  const int seen = min(seen_by(a, u.s, query), end);
   bf16x8_t qf[HD / 16];
   {
     const bf16_t* const Q = (const bf16_t*)a.q + (long)(a.q_off[u.s] + query) * a.ldq + (long)head * HD;
 #pragma unroll
     for (int s = 0; s < HD / 16; ++s) qf[s] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(Q + (s * 2 + hl) * 8));
-#pragma unroll
-    for (int s = 0; s < HD / 16; ++s) asm volatile("" : "+v"(qf[s]));  // here, ahead of the loads that are counted
   }
+  __builtin_amdgcn_sched_barrier(0);
+  const int k0 = u.begin + wave * kFewKeys;
+  load(K, k0, false);
+  load(V, k0, true);
   f32x16_t o[HD / 32] = {};
   float mx = -FLT_MAX, l = 0.f;
   const float sl2 = a.scale * 1.4426950408889634f;
@@ -600,21 +599,29 @@ void grouped_few_kernel(const GroupedArgs a) {
     const int key = hl * 4 + (lane & 15) / 4;
     vf[db] = TILE + key * ROWB + vswz(key, db * 4 + (lane >> 4 & 1) * 2 + (lane & 3) / 2) * 16 + (lane & 1) * 8;
   }
-  auto step = [&](int k0, auto stc) __attribute__((always_inline)) {
-    constexpr int st = decltype(stc)::value;
-    wait_vmcnt<2 * NI>();  // all but the next tile's loads
+#pragma unroll 1
+  for (int k = k0; k < end; k += NW * kFewKeys) {
+    wait_vmcnt<NI>();  // this tile's K; its V may be on its way
     __builtin_amdgcn_sched_barrier(0);
-    f32x16_t s = {};
+    bf16x8_t kr[HD / 16];
 #pragma unroll
-    for (int ks = 0; ks < HD / 16; ++ks) {
-      const bf16x8_t f = __builtin_bit_cast(bf16x8_t, *(const uint4*)(lbase + kf[ks] + st * STAGE));
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[ks], s, 0, 0, 0);
+    for (int ks = 0; ks < HD / 16; ++ks) kr[ks] = __builtin_bit_cast(bf16x8_t, *(const uint4*)(lbase + kf[ks]));
+    wait_lgkmcnt0();  // read, before the next tile's K arrives here
+    __builtin_amdgcn_sched_barrier(0);
+    load(K, k + NW * kFewKeys, false);
+    // two sums, whose products need not wait for each other
+    f32x16_t s = {}, s1 = {};
+#pragma unroll
+    for (int ks = 0; ks < HD / 16; ks += 2) {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr[ks], qf[ks], s, 0, 0, 0);
+      s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr[ks + 1], qf[ks + 1], s1, 0, 0, 0);
     }
-    const bool mask = k0 + kFewKeys > min(least, end);
+    s += s1;
+    const bool mask = k + kFewKeys > least;
     if (mask) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (k0 + (i >> 2) * 8 + hl * 4 + (i & 3) >= min(seen, end)) s[i] = -INFINITY;
+        if (k + (i >> 2) * 8 + hl * 4 + (i & 3) >= seen) s[i] = -INFINITY;
     }
     bf16x8_t pf[2];
     auto probabilities = [&]() __attribute__((always_inline)) {
@@ -656,163 +663,196 @@ void grouped_few_kernel(const GroupedArgs a) {
       t = probabilities();
     }
     l += t;
-    auto v_frag = [&](int g, int db) __attribute__((always_inline)) {
-      bf16x4_t v[2];
+    wait_vmcnt<NI>();  // this tile's V; the next one's K may be on its way
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8_t vr[2][HD / 32];
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
-        v[e] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-            (__attribute__((address_space(3))) bf16x4_t*)(lbase + vf[db] + st * STAGE + (g * 16 + e * 8) * ROWB));
-      return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    bool plain = true;
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int db = 0; db < HD / 32; ++db) {
+        bf16x4_t v[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          v[e] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+              (__attribute__((address_space(3))) bf16x4_t*)(lbase + vf[db] + (g * 16 + e * 8) * ROWB));
+        vr[g][db] = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      }
     if (mask) {
       float z = 0.f;
       const bf16x2_t zero = {(__bf16)0.0f, (__bf16)0.0f};
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
-        for (int db = 0; db < HD / 32; ++db) {
-          const bf16x8_t f = v_frag(g, db);
-#pragma unroll
-          for (int e = 0; e < 8; e += 2) z = __builtin_amdgcn_fdot2_f32_bf16(bf16x2_t{f[e], f[e + 1]}, zero, z, false);
-        }
-      plain = !__any(z != z);
-    }
-    if (plain) {
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int db = 0; db < HD / 32; ++db)
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag(g, db), pf[g], o[db], 0, 0, 0);
-    } else {
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int db = 0; db < HD / 32; ++db) {
-          uint4 w = __builtin_bit_cast(uint4, v_frag(g, db));
-          w = make_uint4(finite_halves(w.x), finite_halves(w.y), finite_halves(w.z), finite_halves(w.w));
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, w), pf[g], o[db], 0, 0, 0);
-        }
-#pragma unroll 1
-      for (int key = 0; key < kFewKeys; ++key) {
-        const int ln = opaque(lane);
-        const int at = (key >> 3) * 4 + (key & 3);
-        uint32_t w = 0;
-        static_for<8>([&](auto ic) {
-          constexpr int i = decltype(ic)::value;
-          const uint4 q = __builtin_bit_cast(uint4, pf[i >> 2]);
-          if (at >> 1 == i) w = (i & 3) == 0 ? q.x : (i & 3) == 1 ? q.y : (i & 3) == 2 ? q.z : q.w;
-        });
-        const float pr = __shfl(__uint_as_float(at & 1 ? w & 0xffff0000 : w << 16), (ln & 31) | (key >> 2 & 1) << 5, 64);
-        const bool in = k0 + key < min(seen, end);
-#pragma unroll
         for (int db = 0; db < HD / 32; ++db)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int dim = db * 32 + q * 8 + (ln >> 5) * 4;
-            const uint2 v = *(const uint2*)(lbase + st * STAGE + TILE + key * ROWB + vswz(key, dim / 8) * 16 + dim % 8 * 2);
-            const float f[4] = {__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000), __uint_as_float(v.y << 16),
-                                __uint_as_float(v.y & 0xffff0000)};
+          for (int e = 0; e < 8; e += 2)
+            z = __builtin_amdgcn_fdot2_f32_bf16(bf16x2_t{vr[g][db][e], vr[g][db][e + 1]}, zero, z, false);
+      if (__any(z != z)) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (in && !is_finite(f[r])) o[db][q * 4 + r] = fmaf(pr, f[r], o[db][q * 4 + r]);
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int db = 0; db < HD / 32; ++db) {
+            const uint4 w = __builtin_bit_cast(uint4, vr[g][db]);
+            vr[g][db] = __builtin_bit_cast(
+                bf16x8_t, make_uint4(finite_halves(w.x), finite_halves(w.y), finite_halves(w.z), finite_halves(w.w)));
           }
+#pragma unroll 1
+        for (int key = 0; key < kFewKeys; ++key) {
+          // the row's probability of this key: register (key / 8) * 4 + key % 4 of lane half key / 4 % 2
+          const int ln = opaque(lane), at = (key >> 3) * 4 + (key & 3);
+          uint32_t w = 0;
+          static_for<8>([&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            const uint4 q = __builtin_bit_cast(uint4, pf[i >> 2]);
+            if (at >> 1 == i) w = (i & 3) == 0 ? q.x : (i & 3) == 1 ? q.y : (i & 3) == 2 ? q.z : q.w;
+          });
+          const float pr = __shfl(__uint_as_float(at & 1 ? w & 0xffff0000 : w << 16), (ln & 31) | (key >> 2 & 1) << 5, 64);
+          const bool in = k + key < seen;
+#pragma unroll
+          for (int db = 0; db < HD / 32; ++db)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int dim = db * 32 + q * 8 + (ln >> 5) * 4;
+              const uint2 v = *(const uint2*)(lbase + TILE + key * ROWB + vswz(key, dim / 8) * 16 + dim % 8 * 2);
+              const float f[4] = {__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000), __uint_as_float(v.y << 16),
+                                  __uint_as_float(v.y & 0xffff0000)};
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                o[db][q * 4 + r] = fmaf(pr, in && !is_finite(f[r]) ? f[r] : 0.f, o[db][q * 4 + r]);
+            }
+        }
       }
     }
-    wait_lgkmcnt0();  // read, before the tile after the next arrives here
+    wait_lgkmcnt0();  // read, before the next tile's V arrives here
     __builtin_amdgcn_sched_barrier(0);
-    tile_load(k0 + 2 * NW * kFewKeys, st);
-  };
-  using S0 = std::integral_constant<int, 0>;
-  using S1 = std::integral_constant<int, 1>;
-  const int k0 = u.begin + wave * kFewKeys;
-  tile_load(k0, 0);
-  tile_load(k0 + NW * kFewKeys, 1);
-#pragma unroll 1
-  for (int k = k0; k < end; k += 2 * NW * kFewKeys) {
-    step(k, S0{});
-    if (k + NW * kFewKeys < end) step(k + NW * kFewKeys, S1{});
+    load(V, k + NW * kFewKeys, true);
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int db = 0; db < HD / 32; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vr[g][db], pf[g], o[db], 0, 0, 0);
   }
   wait_vmcnt<0>();
   l += __shfl_xor(l, 32, 64);
-  // the second wave's results over the first's tiles, which are read no more
-  constexpr int NR = HD / 2;
-  static_assert((NR + 2) * 64 * 4 <= NW * 2 * STAGE, "merge LDS");
+  // All waves' results over the tiles, which are read no more; wave w joins dimensions 32 w .. in wave order.  A wave
+  // without a key has the lowest max, sum 0 and O 0.
   __syncthreads();
   float* const sh = (float*)smem + lane;
-  if (wave == 1) {
+  {
+    float* const to = sh + wave * (NR + 2) * 64;
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sh[(d * 16 + i) * 64] = o[d][i];
-    sh[NR * 64] = mx;
-    sh[(NR + 1) * 64] = l;
+      for (int i = 0; i < 16; ++i) to[(d * 16 + i) * 64] = o[d][i];
+    to[NR * 64] = mx;
+    to[(NR + 1) * 64] = l;
   }
   __syncthreads();
-  if (wave == 1 || row > last) return;
-  // a wave without a key has the lowest max, sum 0 and O 0
-  const float m1 = sh[NR * 64], mm = fmaxf(mx, m1);
-  const float a0 = __builtin_amdgcn_exp2f(mx - mm), a1 = __builtin_amdgcn_exp2f(m1 - mm);
-  l = l * a0 + sh[(NR + 1) * 64] * a1;
+  if (wave >= HD / 32 || row > last) return;
+  float mm = sh[NR * 64], sum = 0.f;
 #pragma unroll
-  for (int d = 0; d < HD / 32; ++d)
+  for (int w = 1; w < NW; ++w) mm = fmaxf(mm, sh[(w * (NR + 2) + NR) * 64]);
+  float y[16] = {};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * a0 + sh[(d * 16 + i) * 64] * a1;
+  for (int w = 0; w < NW; ++w) {
+    const float* const from = sh + w * (NR + 2) * 64;
+    const float al = __builtin_amdgcn_exp2f(from[NR * 64] - mm);
+    sum = fmaf(al, from[(NR + 1) * 64], sum);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = fmaf(al, from[(wave * 16 + i) * 64], y[i]);
+  }
   if (u.ranges > 1) {
-    float* const po = part_o(a, id, kFewRows) + (long)row * HD;
+    float* const po = part_o(a, id, kFewRows) + (long)row * HD + wave * 32 + hl * 4;
 #pragma unroll
-    for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *(float4*)(po + d * 32 + g * 8 + hl * 4) = make_float4(o[d][g * 4], o[d][g * 4 + 1], o[d][g * 4 + 2], o[d][g * 4 + 3]);
-    if (hl == 0) part_ml(a, id, kFewRows)[row] = make_float2(mm, l);
+    for (int g = 0; g < 4; ++g) *(float4*)(po + g * 8) = make_float4(y[g * 4], y[g * 4 + 1], y[g * 4 + 2], y[g * 4 + 3]);
+    if (wave == 0 && hl == 0) part_ml(a, id, kFewRows)[row] = make_float2(mm, sum);
     return;
   }
-  const float inv = seen > 0 ? 1.0f / l : 0.f;
-  bf16_t* const og = (bf16_t*)a.o + (long)(a.q_off[u.s] + query) * a.ldo + (long)head * HD;
+  const float inv = seen > 0 ? 1.0f / sum : 0.f;
+  bf16_t* const og = (bf16_t*)a.o + (long)(a.q_off[u.s] + query) * a.ldo + (long)head * HD + wave * 32 + hl * 4;
 #pragma unroll
-  for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      uint2 w;
-      w.x = pack_bf16x2(o[d][g * 4 + 0] * inv, o[d][g * 4 + 1] * inv);
-      w.y = pack_bf16x2(o[d][g * 4 + 2] * inv, o[d][g * 4 + 3] * inv);
-      *(uint2*)(og + d * 32 + g * 8 + hl * 4) = w;
-    }
+  for (int g = 0; g < 4; ++g) {
+    uint2 w;
+    w.x = pack_bf16x2(y[g * 4 + 0] * inv, y[g * 4 + 1] * inv);
+    w.y = pack_bf16x2(y[g * 4 + 2] * inv, y[g * 4 + 3] * inv);
+    *(uint2*)(og + g * 8) = w;
+  }
 }
 
 // ---------------------------------------------------------------- ranges of keys joined
-// The ranges of a tile of `per` rows, in their order: 8 rows at a time, HD / 4 threads a
-// row.  The block of a tile's first range does it.
-template <typename T, int HD>
+// A row's ranges in their order; `t` of the HD / 4 threads that take 4 dimensions each.  FEW: tiles of kFewRows rows, one to
+// a sequence, whose ranges may be many: a block takes one row, and its 8 groups of threads every 8th range each, which meet
+// in LDS.  Otherwise the block of a tile's first range takes the tile, 8 rows at a time.
+struct Joined {
+  float m, l;
+  float4 y;
+};
+__device__ __forceinline__ Joined join_ranges(const float2* ml, const float* po, long ml_step, long o_step, int from, int to, int by) {
+  Joined j = {-FLT_MAX, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 4
+  for (int i = from; i < to; i += by) j.m = fmaxf(j.m, ml[i * ml_step].x);
+#pragma unroll 4
+  for (int i = from; i < to; i += by) {
+    const float2 x = ml[i * ml_step];
+    const float4 v = *(const float4*)(po + i * o_step);
+    const float al = exp2f(x.x - j.m);
+    j.l = fmaf(al, x.y, j.l);
+    j.y = make_float4(fmaf(al, v.x, j.y.x), fmaf(al, v.y, j.y.y), fmaf(al, v.z, j.y.z), fmaf(al, v.w, j.y.w));
+  }
+  return j;
+}
+
+template <typename T, int HD, bool FEW>
 __global__ __launch_bounds__(HD * 2) void grouped_merge_kernel(const GroupedArgs a, int per) {
-  const int id = block_id();
-  if (id >= a.tile_off[a.n_seq] * a.kv_heads) return;
-  const Unit u = unit_of(a, id, per);
-  if (u.ranges == 1 || u.begin > 0) return;
-  const int dd = threadIdx.x % (HD / 4) * 4;
-  for (int r = threadIdx.x / (HD / 4); r < per && u.row0 + r < u.rows; r += 8) {
-    // the ranges of a tile are kv_heads units apart
-    const float2* const ml = part_ml(a, id, per) + r;
-    const float* const po = part_o(a, id, per) + (long)r * HD + dd;
-    const long ml_step = (long)a.kv_heads * per, o_step = ml_step * HD;
-    float m = -FLT_MAX, l = 0.f;
+  constexpr int TPR = HD / 4, GROUPS = 8;
+  __shared__ float4 part_y[FEW ? GROUPS : 1][TPR];
+  __shared__ float2 part_m[FEW ? GROUPS : 1];
+  int id = block_id();
+  const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+  if constexpr (FEW) {
+    const int s = id / (a.kv_heads * kFewRows), h = id / kFewRows % a.kv_heads;
+    if (s >= a.n_seq) return;
+    const int row = id % kFewRows;
+    id = a.tile_off[s] * a.kv_heads + h;
+    const Unit u = unit_of(a, id, per);
+    if (u.ranges == 1 || row >= u.rows) return;
+    const long ml_step = (long)a.kv_heads * per, o_step = ml_step * HD;  // a tile's ranges are kv_heads units apart
+    const Joined j = join_ranges(part_ml(a, id, per) + row, part_o(a, id, per) + (long)row * HD + t * 4, ml_step, o_step, g,
+                                 u.ranges, GROUPS);
+    part_y[g][t] = j.y;
+    if (t == 0) part_m[g] = make_float2(j.m, j.l);
+    __syncthreads();
+    if (g > 0) return;
+    float m = part_m[0].x, l = 0.f;
+#pragma unroll
+    for (int i = 1; i < GROUPS; ++i) m = fmaxf(m, part_m[i].x);
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = 0; i < u.ranges; ++i) {
-      const float2 x = ml[i * ml_step];
-      const float4 v = *(const float4*)(po + i * o_step);
-      const float mm = fmaxf(m, x.x), a0 = exp2f(m - mm), a1 = exp2f(x.x - mm);
-      m = mm;
-      l = l * a0 + x.y * a1;
-      y = make_float4(y.x * a0 + v.x * a1, y.y * a0 + v.y * a1, y.z * a0 + v.z * a1, y.w * a0 + v.w * a1);
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {  // a group without a range has the lowest max, and zeros
+      const float al = exp2f(part_m[i].x - m);
+      const float4 v = part_y[i][t];
+      l = fmaf(al, part_m[i].y, l);
+      y = make_float4(fmaf(al, v.x, y.x), fmaf(al, v.y, y.y), fmaf(al, v.z, y.z), fmaf(al, v.w, y.w));
     }
-    const int row = u.row0 + r, query = row / a.group;
+    const int query = row / a.group;
     const float inv = seen_by(a, u.s, query) > 0 ? 1.0f / l : 0.f;
-    T* const o = (T*)a.o + (long)(a.q_off[u.s] + query) * a.ldo + (long)(u.h * a.group + row - query * a.group) * HD + dd;
-    if constexpr (sizeof(T) == 2)
-      *(uint2*)o = make_uint2(pack_bf16x2(y.x * inv, y.y * inv), pack_bf16x2(y.z * inv, y.w * inv));
-    else
-      *(float4*)o = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+    T* const o = (T*)a.o + (long)(a.q_off[u.s] + query) * a.ldo + (long)(u.h * a.group + row - query * a.group) * HD + t * 4;
+    *(uint2*)o = make_uint2(pack_bf16x2(y.x * inv, y.y * inv), pack_bf16x2(y.z * inv, y.w * inv));
+  } else {
+    if (id >= a.tile_off[a.n_seq] * a.kv_heads) return;
+    const Unit u = unit_of(a, id, per);
+    if (u.ranges == 1 || u.begin > 0) return;
+    const long ml_step = (long)a.kv_heads * per, o_step = ml_step * HD;
+    for (int r = g; r < per && u.row0 + r < u.rows; r += GROUPS) {
+      const Joined j = join_ranges(part_ml(a, id, per) + r, part_o(a, id, per) + (long)r * HD + t * 4, ml_step, o_step, 0,
+                                   u.ranges, 1);
+      const int row = u.row0 + r, query = row / a.group;
+      const float inv = seen_by(a, u.s, query) > 0 ? 1.0f / j.l : 0.f;
+      T* const o = (T*)a.o + (long)(a.q_off[u.s] + query) * a.ldo + (long)(u.h * a.group + row - query * a.group) * HD + t * 4;
+      if constexpr (sizeof(T) == 2)
+        *(uint2*)o = make_uint2(pack_bf16x2(j.y.x * inv, j.y.y * inv), pack_bf16x2(j.y.z * inv, j.y.w * inv));
+      else
+        *(float4*)o = make_float4(j.y.x * inv, j.y.y * inv, j.y.z * inv, j.y.w * inv);
+    }
   }
 }
 
@@ -826,16 +866,18 @@ struct Plan {
 enum Kind { ROWS, FEW, F32 };
 
 // The sequences of `in` that `kind` takes, cut into ranges where the launch is then modelled to end sooner.
-// A block's time goes with its 64-key steps, and a launch's with the longest block or with all steps over the blocks that
-// run at a time; ranges cost the merge and their partial results' way to memory and back.
-Plan plan_of(const GroupedArgs& in, Kind kind) {
+constexpr size_t kMostBytes = 128 << 20;
+Plan plan_of(const GroupedArgs& in, Kind kind, bool may_cut = true) {
   Plan p;
   p.a = in;
   GroupedArgs& a = p.a;
   p.per = kind == F32 ? FQ : kind == FEW ? kFewRows : 128;
+  // sequences of few rows have a kernel of their own, unless they are short and the other one is launched anyway
+  bool many = false;
+  for (int i = 0; i < in.n_seq; ++i) many = many || (long)in.q_len[i] * in.group > kFewRows;
   a.n_seq = 0;
   for (int i = 0; i < in.n_seq; ++i) {
-    const bool few = (long)in.q_len[i] * in.group <= kFewRows;
+    const bool few = (long)in.q_len[i] * in.group <= kFewRows && !(many && in.kv_len[i] <= 2048);
     if (in.q_len[i] == 0 || (kind == FEW && !few) || (kind == ROWS && few)) continue;
     a.q_off[a.n_seq] = in.q_off[i];
     a.q_len[a.n_seq] = in.q_len[i];
@@ -843,50 +885,34 @@ Plan plan_of(const GroupedArgs& in, Kind kind) {
     a.kv_row[a.n_seq] = in.kv_row[i];
     ++a.n_seq;
   }
-  p.units = 0;
-  p.bytes = 0;
-  // us of a step: alone in a block, and with all CUs at work (blocks of few rows then wait for memory)
-  const double alone = kind == FEW ? 0.8 : a.head_dim == 64 ? 0.6 : 0.8;
-  const double busy = kind == FEW ? a.head_dim * 256 / 5e6 : kind == F32 ? 2.0 / 768 : a.head_dim == 64 ? 1.5 / 768 : 1.6 / 512;
-  double best = 1e30;
-  int best_chunk = 1 << 30;
-  for (int c = 1 << 25; c >= 256; c /= 2) {
-    double steps = 0, longest = 0, units = 0, cut = 0;
-    for (int i = 0; i < a.n_seq; ++i) {
-      const double tiles = (double)(((long)a.q_len[i] * a.group + p.per - 1) / p.per) * a.kv_heads, keys = a.kv_len[i];
-      const double first = a.causal ? fmax(keys - a.q_len[i], 0.0) : keys;  // seen by the first query
-      steps += tiles * ((first + keys) / 128 + 1);
-      longest = fmax(longest, fmin(keys, c) / 64);
-      const double n = tiles * ceil(fmax(keys, 1.0) / c);
-      units += n;
-      if (keys > c) cut += n;
-    }
-    const double unit_bytes = p.per * (a.head_dim + 2) * 4.0;
-    const double us = fmax(longest * alone, steps * busy) + (cut > 0 ? 4.0 + 2 * cut * unit_bytes / 4e6 : 0.0);
-    if (us < best && (cut == 0 || units * unit_bytes < 128e6)) {
-      best = us;
-      best_chunk = c;
-    }
-  }
-  a.chunk = best_chunk;
-  a.tile_off[0] = 0;
-  long parts = 0;
+  // Ranges as long as what one of 512 blocks (two to a CU) takes if all take the same.
+  constexpr int kWhole = 1 << 30;
+  double keys = 0;
+  int longest = 0;
   for (int i = 0; i < a.n_seq; ++i) {
-    const long n = ((long)a.q_len[i] * a.group + p.per - 1) / p.per * ranges_of(a, i);
-    a.tile_off[i + 1] = a.tile_off[i] + (int)n;
-    if (ranges_of(a, i) > 1) parts += n;
+    keys += (double)(((long)a.q_len[i] * a.group + p.per - 1) / p.per) * a.kv_heads * a.kv_len[i];
+    longest = std::max(longest, a.kv_len[i]);
+  }
+  const double even = fmax(keys / 512 * (kind == ROWS ? 2 : 1), kind == ROWS ? 2048 : 256);
+  a.chunk = !may_cut || longest <= 768 || even >= longest ? kWhole : ((int)even + kKeys - 1) / kKeys * kKeys;
+  a.tile_off[0] = 0;
+  bool cut = false;
+  for (int i = 0; i < a.n_seq; ++i) {
+    a.tile_off[i + 1] = a.tile_off[i] + (int)(((long)a.q_len[i] * a.group + p.per - 1) / p.per * ranges_of(a, i));
+    cut = cut || ranges_of(a, i) > 1;
   }
   p.units = (long)a.tile_off[a.n_seq] * a.kv_heads;
-  if (parts > 0) p.bytes = (size_t)p.units * p.per * (a.head_dim + 2) * 4;
+  p.bytes = cut ? (size_t)p.units * p.per * (a.head_dim + 2) * 4 : 0;
+  if (p.bytes > kMostBytes) return plan_of(in, kind, false);
   return p;
 }
 
-template <typename T>
+template <typename T, bool FEW_ROWS>
 void launch_merge(const Plan& p, hipStream_t s) {
   if (p.bytes == 0) return;
-  const dim3 grid = grid_of(p.units);
-  if (p.a.head_dim == 64) hipLaunchKernelGGL((grouped_merge_kernel<T, 64>), grid, dim3(128), 0, s, p.a, p.per);
-  else hipLaunchKernelGGL((grouped_merge_kernel<T, 128>), grid, dim3(256), 0, s, p.a, p.per);
+  const dim3 grid = grid_of(FEW_ROWS ? (long)p.a.n_seq * p.a.kv_heads * kFewRows : p.units);
+  if (p.a.head_dim == 64) hipLaunchKernelGGL((grouped_merge_kernel<T, 64, FEW_ROWS>), grid, dim3(128), 0, s, p.a, p.per);
+  else hipLaunchKernelGGL((grouped_merge_kernel<T, 128, FEW_ROWS>), grid, dim3(256), 0, s, p.a, p.per);
 }
 
 }  // namespace
@@ -906,22 +932,22 @@ hipError_t launch_attention_grouped(int dtype, const GroupedArgs& a, hipStream_t
     const Plan p = plan_of(a, F32);
     if (p.units == 0) return hipSuccess;
     hipLaunchKernelGGL(grouped_f32_kernel, grid_of(p.units), dim3(256), 0, s, p.a);
-    launch_merge<float>(p, s);
+    launch_merge<float, false>(p, s);
     return hipGetLastError();
   }
   // one kernel after the other on the stream, and so on one workspace
   const Plan few = plan_of(a, FEW), rows = plan_of(a, ROWS);
   if (few.units > 0) {
     const dim3 grid = grid_of(few.units);
-    if (a.head_dim == 64) hipLaunchKernelGGL((grouped_few_kernel<64>), grid, dim3(128), 0, s, few.a);
-    else hipLaunchKernelGGL((grouped_few_kernel<128>), grid, dim3(128), 0, s, few.a);
-    launch_merge<bf16_t>(few, s);
+    if (a.head_dim == 64) hipLaunchKernelGGL((grouped_few_kernel<64>), grid, dim3(kFewWaves * 64), 0, s, few.a);
+    else hipLaunchKernelGGL((grouped_few_kernel<128>), grid, dim3(kFewWaves * 64), 0, s, few.a);
+    launch_merge<bf16_t, true>(few, s);
   }
   if (rows.units > 0) {
     const dim3 grid = grid_of(rows.units);
     if (a.head_dim == 64) hipLaunchKernelGGL((grouped_bf16_kernel<64>), grid, dim3(256), 0, s, rows.a);
     else hipLaunchKernelGGL((grouped_bf16_kernel<128>), grid, dim3(256), 0, s, rows.a);
-    launch_merge<bf16_t>(rows, s);
+    launch_merge<bf16_t, false>(rows, s);
   }
   return hipGetLastError();
 }
