@@ -1315,7 +1315,7 @@ dit_status dit_linear_fp4(int M, int N, int K, const void* x_codes, const void* 
     return fail(DIT_ERR_INVALID_ARG, "b / y is not aligned to its elements");
   hipStream_t s = (hipStream_t)stream;
   const double bytes = ((double)M + N) * (fp4_pitch(K) + fp4_scale_pitch(K)) + (double)M * N * elem_size(out_dtype);
-  HIP_TRY(timed(s, gemm_fp4_config_name(M, N, K, out_dtype), 2.0 * M * N * (double)K, bytes, [&] {
+  HIP_TRY(timed(s, gemm_fp4_config_name(M, N, K), 2.0 * M * N * (double)K, bytes, [&] {
     return launch_gemm_fp4(M, N, K, x_codes, x_scales, w_codes, w_scales, b, b_dtype, y, out_dtype, s);
   }));
   return DIT_OK;

@@ -308,7 +308,7 @@ hipError_t launch_dequantize_fp4(int dtype, const void* q, const void* scales, l
 hipError_t launch_gemm_fp4(int M, int N, int K, const void* x, const void* xs, const void* w, const void* ws,
                            const void* bias, int bias_dtype, void* y, int out_dtype, hipStream_t s);
 // name of the kernel launch_gemm_fp4 picks
-const char* gemm_fp4_config_name(int M, int N, int K, int out_dtype);
+const char* gemm_fp4_config_name(int M, int N, int K);
 
 // rotary positions; w: host array of rot / 2 angles per position
 hipError_t launch_rope(int dtype, long rows, int heads, int d, int rot, int layout, const int* pos, const double* w,

@@ -54,24 +54,25 @@ __device__ __forceinline__ int opaque(int v) {
   return v;
 }
 __device__ __forceinline__ void block_barrier() { asm volatile("s_barrier" ::: "memory"); }
-// c += w x of 64 elements, the scales in byte B of their words.  A volatile statement: as a builtin the compiler moves it
-// out of its turn between two barriers.  It does not see what the statement is: nothing may write an operand by vector
-// arithmetic, nor read c, within the instruction's wait states.
+// c += w x (first: c = w x) of 64 elements, the scales in byte B of their words.  Volatile statements, which keep their
+// places among the reads and loads between them.  The compiler does not see what they are: nothing may read c within the
+// instruction's wait states.
+#define FP4_MFMA(OUT, C, SEL)                                                                                         \
+  asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, " C ", %3, %4 " SEL " cbsz:4 blgp:4"                      \
+               : OUT(c)                                                                                               \
+               : "v"(w), "v"(x), "v"(sw), "v"(sx))
+#define FP4_MFMA_BYTES(OUT, C)                                                        \
+  if constexpr (B == 0) FP4_MFMA(OUT, C, "op_sel:[0,0,0] op_sel_hi:[0,0,0]");          \
+  else if constexpr (B == 1) FP4_MFMA(OUT, C, "op_sel:[1,1,0] op_sel_hi:[0,0,0]");     \
+  else if constexpr (B == 2) FP4_MFMA(OUT, C, "op_sel:[0,0,0] op_sel_hi:[1,1,0]");     \
+  else FP4_MFMA(OUT, C, "op_sel:[1,1,0] op_sel_hi:[1,1,0]")
 template <int B>
 __device__ __forceinline__ void asm_mfma(f32x16_t& c, const i32x4_t& w, const i32x4_t& x, int sw, int sx) {
-  static_assert(B >= 0 && B < 4, "scale byte");
-  if constexpr (B == 0)
-    asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4"
-                 : "+v"(c) : "v"(w), "v"(x), "v"(sw), "v"(sx));
-  else if constexpr (B == 1)
-    asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4"
-                 : "+v"(c) : "v"(w), "v"(x), "v"(sw), "v"(sx));
-  else if constexpr (B == 2)
-    asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[1,1,0] cbsz:4 blgp:4"
-                 : "+v"(c) : "v"(w), "v"(x), "v"(sw), "v"(sx));
-  else
-    asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[1,1,0] cbsz:4 blgp:4"
-                 : "+v"(c) : "v"(w), "v"(x), "v"(sw), "v"(sx));
+  FP4_MFMA_BYTES("+a", "%0");
+}
+template <int B>
+__device__ __forceinline__ void asm_mfma_first(f32x16_t& c, const i32x4_t& w, const i32x4_t& x, int sw, int sx) {
+  FP4_MFMA_BYTES("=a", "0");
 }
 
 // grouped order: 8 M-tiles share each run of N-tiles, for L2 reuse of both operands
@@ -113,35 +114,74 @@ __device__ __forceinline__ void store_columns(char* y, const float* v, int left)
   }
 }
 
+// 16 bytes of an output row that ends `left` columns further, at any element's address.  Past the caches: the 256x256 tiles'
+// outputs, written line by line, would push the operands out of them (N = 16384, K = 4096: 572 us for 606).
+template <bool F32>
+__device__ __forceinline__ void store_chunk(char* y, const u32x4_t& w, int left) {
+  constexpr int C = F32 ? 4 : 8;
+  if (left >= C) {
+    __builtin_nontemporal_store(w, &((Bf16x8*)y)->v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < C - 1; ++i)
+      if (i < left) {
+        if constexpr (F32) ((uint32_t*)y)[i] = w[i];
+        else ((uint16_t*)y)[i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
+      }
+  }
+}
+// Lanes that differ in bits 3 and 4 and four registers change places: register k of lane (8 a + l), a < 4, is what register a
+// of lane (8 k + l) was.
+__device__ __forceinline__ void turn4(u32x4_t (&w)[4]) {
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    uint32_t r[4];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const auto s = __builtin_amdgcn_permlane16_swap(w[k][d], w[k + 2][d], false, false);
+      r[k] = s[0];
+      r[k + 2] = s[1];
+    }
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {  // row_ror:8, the upper or lower 8 lanes of each 16
+      w[k][d] = __builtin_amdgcn_update_dpp(r[k], r[k + 1], 0x128, 0xf, 0xc, false);
+      w[k + 1][d] = __builtin_amdgcn_update_dpp(r[k + 1], r[k], 0x128, 0xf, 0x3, false);
+    }
+  }
+}
+
 // ---------------------------------------------------------------- 256 x 256 tiles
 constexpr int kMaxBlocks256 = 256;  // one per CU
 constexpr int kMinKTiles256 = 3;    // its loads run up to three K tiles ahead, into the next output tile at most
 
-// 8 waves, each 128 rows x 64 columns, by 32x32x64 matrix instructions.  K tiles of 128
-// bytes (256 elements) move by direct-to-LDS loads into two stages.  Two wave groups
-// (waves 0-3 and 4-7, one wave of each per SIMD) take turns: while one issues a cluster
-// of 8 MFMAs, the other reads the fragments of its next cluster from LDS and issues its
-// share of the loads; block barriers hold the groups one turn apart.  A K tile is 4
-// clusters: cluster c multiplies the wave's c-th 32 rows of X with all its 64 rows of W
-// (2 fragments of 4 steps each, held for a whole tile, two tiles in turn).  Read phase 4
-// kt + c takes the X of the next cluster, 4 kt + c + 1, and of W of tile kt + 1 fragment
-// c / 2, steps 2 (c % 2) and the next; every wave has their data ahead of the first
-// barrier of its next phase, which the other group meets a turn later.  So a place is
-// loaded again two phases after its last read: X's part c of tile kt + 2 in phase 4 kt +
-// c + 1; W's parts 0 and 1, which hold fragment 0, of tile kt + 3 in phase 4 kt + 3, its
-// parts 2 and 3, fragment 1, in phase 4 kt + 5.  X is read 6 phases after its load, W 5:
-// loads have 4 phases until the wait that makes them visible.
+// 4 waves, one per SIMD, each 128 rows x 128 columns by 32x32x64 matrix instructions: 16
+// sums of 16 registers each, in accumulation registers.  K tiles of 128 bytes (256
+// elements) move by direct-to-LDS loads into two stages, each in parts: X's part c holds
+// the c-th 32 rows of either wave row, W's part j fragment j of either wave column.  A K
+// tile is 4 phases: phase c multiplies the wave's c-th 32 rows of X with all its rows of
+// W (4 fragments of 4 steps, held for a whole tile, two tiles in turn), and between its
+// 16 MFMAs reads the X of the next phase, fragment c of W of the next K tile, and issues
+// its share of the loads.  One barrier ends a phase; ahead of it a wave's reads have
+// returned, so a place is loaded again in the phase after its read: in phase 4 kt + c
+// X's part c of tile kt + 2, and W's part c - 1 of tile kt + 3 (c = 0: part 3 of kt + 2).
+// Both are read 7 phases after their load: loads have 6 phases.
 // A block works through its output tiles as one stream of K tiles: the loads of the next
-// output tile run ahead of the last K tiles of this one, and each cluster's finished sums
-// are written in its read phase of the next tile's first K tile, beside the other group's
-// MFMAs.  W's rows are dealt out to the fragments so that a lane holds 32 neighbouring
-// columns of a row: it writes them straight from registers.
+// output tile run ahead of the last K tiles of this one.  The finished sums of rows c are
+// written between the MFMAs of the phase ahead of the one that starts them anew: rows 0
+// in the last phase of the tile, 1 to 3 in the first three of the next.  W's rows are
+// dealt out to the fragments so that a lane's and its neighbour's 16-byte chunks lie
+// side by side; four chunks change places with those of the lanes of three other rows,
+// and a store writes 128 bytes of each of 8 rows (16 bytes of each of 64 took 1068 us
+// for 606 at 16896 x 16384 x 4096).
+// 8192^3 248 us, 4.4 PFLOP/s; 16717 x 4096 x 16384 515 us; 16896 x 16384 x 4096 571 us;
+// the same instructions without loads reach 6.7.  8 waves of 128 x 64, two on a SIMD, 268,
+// 555 and 667 us: they read half as much again of LDS.  Here a phase's MFMAs issue back to
+// back; its barrier, and the start and end of a block's work, take the rest.
 template <bool F32>
-__global__ __launch_bounds__(512) void fp4_256_kernel(const Fp4Problem p) {
-  constexpr int BM = 256, BN = 256, Q = 4, NS = F32 ? 8 : 4;  // NS: stores of a phase
-  constexpr int ROWB = 128, CPR = 8, RPI = 8;  // bytes and 16-byte chunks of a row, rows per wave load
+__global__ __launch_bounds__(256) void fp4_256_kernel(const Fp4Problem p) {
+  constexpr int BM = 256, BN = 256, Q = 4, NS = F32 ? 16 : 8;  // NS: stores of a phase
+  constexpr int ROWB = 128;
   constexpr int STAGE = BM * ROWB, SUB = STAGE / Q, REGION = 2 * STAGE;
-  static_assert(BM == BN, "one stage size");
   // [X stage 0, 1 | W stage 0, 1 | scales stage 0, 1: 16 bytes of every row of X, then of W | bias of the last two output
   // tiles]
   constexpr int SCALES = 2 * REGION, SCALE_STAGE = 8192, BIAS = SCALES + 2 * SCALE_STAGE, BIAS_STAGE = 1024;
@@ -153,20 +193,22 @@ __global__ __launch_bounds__(512) void fp4_256_kernel(const Fp4Problem p) {
   const int tile_end = (xcd + 1) * per + min(xcd + 1, rem), tile_step = ((int)gridDim.x - xcd + 7) >> 3;
   int tile_next = xcd * per + min(xcd, rem) + (blockIdx.x >> 3);
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wv >> 2, wn = wv & 3;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wv >> 1, wn = wv & 1;
   // K tiles, and those of an output tile: an even number, the last one of zeros where K has an odd number
   const int KT = p.kt, Kp = p.pitch, KE = (KT + 1) & ~1;
   const int my_tiles = (tile_end - tile_next + tile_step - 1) / tile_step;
 
   // LDS slot of chunk c of row r: 16 consecutive rows' chunks lie in 16 different 16-byte bank groups
   auto swz = [](int row, int c) { return c ^ ((row >> 1) & 7); };
-  // byte offsets of this lane's row of a part; the part and the K tile travel in the scalar offset, which the
-  // range check counts.  X's part c: rows 32 c .. of either wave row.  W's part c: fragment c / 2 of wave columns 2 (c % 2)
-  // and the next, row i of it being column 32 (i / 4 % 2) + 16 (c / 2) + 4 (i / 8) + i % 4 of its wave's 64.
-  const int lrow = wv * RPI + lane / CPR, lc = swz(lrow, lane % CPR) * 16;
-  const int gx = (int)((uint32_t)(lrow / 32 * 128 + lrow % 32) * (uint32_t)Kp + lc);
-  const int gw = (int)((uint32_t)(lrow / 32 * 64 + (lrow >> 2 & 1) * 32 + (lrow % 32 >> 3) * 4 + lrow % 4) * (uint32_t)Kp + lc);
-  const int gs = (wv % 4 * 64 + lane) * p.spitch;
+  // Byte offsets of this lane's row in the first of a wave's two loads of a part; the second takes rows 8 further, whose
+  // slots differ in bit 2.  The part and the K tile travel in the scalar offset, which the range check counts.  Row i of
+  // W's fragment j is column column(j) + HALF (i / 4 % 2) + 4 (i / 8) + i % 4 of its wave's 128.
+  constexpr int HALF = F32 ? 16 : 32;
+  constexpr auto column = [](int j) { return F32 ? j * 32 : j / 2 * 64 + j % 2 * 16; };
+  const int lrow = wv * 16 + lane / 8, li = lrow & 31, lc = swz(lrow, lane % 8) * 16;
+  const int gx = (int)((uint32_t)(lrow / 32 * 128 + li) * (uint32_t)Kp + lc);
+  const int gw = (int)((uint32_t)(lrow / 32 * 128 + (li >> 2 & 1) * HALF + (li >> 3) * 4 + (li & 3)) * (uint32_t)Kp + lc);
+  const int gs = (wv * 64 + lane) * p.spitch;
   // Three streams of loads, X, W and scales, each at a K tile of an output tile of its own; a row that does not exist
   // reads as zeros.
   auto buffer = [](const uint8_t* base, int n) __attribute__((always_inline)) {
@@ -188,20 +230,21 @@ __global__ __launch_bounds__(512) void fp4_256_kernel(const Fp4Problem p) {
   m0_next = m0;
   n0_next = n0;
   int xm = m0, wn0 = n0, xk = 0, wk = 0;
+  // half e of part c of the stream's K tile
   // (locals, not expressions, as the builtins' arguments: the host pass drops the kernel's launch stub otherwise)
-  auto load_x = [&](auto stc, auto cc) __attribute__((always_inline)) {  // part c
-    constexpr int st = decltype(stc)::value, c = decltype(cc)::value;
-    const int vo = gx, so = xk * ROWB + c * 32 * Kp;
+  auto load_x = [&](auto stc, auto cc, auto ec) __attribute__((always_inline)) {
+    constexpr int st = decltype(stc)::value, c = decltype(cc)::value, e = decltype(ec)::value;
+    const int vo = gx ^ (e * 64), so = xk * ROWB + (c * 32 + e * 8) * Kp;
     const __amdgpu_buffer_rsrc_t r = rows(p.x, xm, xk < KT ? BM : 0, p.M, Kp);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        r, (__attribute__((address_space(3))) void*)(lbase + st * STAGE + c * SUB + wv * RPI * ROWB), 16, vo, so, 0, 0);
+        r, (__attribute__((address_space(3))) void*)(lbase + st * STAGE + c * SUB + (wv * 2 + e) * 1024), 16, vo, so, 0, 0);
   };
-  auto load_w = [&](auto stc, auto cc) __attribute__((always_inline)) {
-    constexpr int st = decltype(stc)::value, c = decltype(cc)::value;
-    const int vo = gw, so = wk * ROWB + ((c & 1) * 128 + (c >> 1) * 16) * Kp;
+  auto load_w = [&](auto stc, auto jc, auto ec) __attribute__((always_inline)) {
+    constexpr int st = decltype(stc)::value, j = decltype(jc)::value, e = decltype(ec)::value;
+    const int vo = gw ^ (e * 64), so = wk * ROWB + (column(j) + e * 4) * Kp;
     const __amdgpu_buffer_rsrc_t r = rows(p.w, wn0, wk < KT ? BN : 0, p.N, Kp);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        r, (__attribute__((address_space(3))) void*)(lbase + REGION + st * STAGE + c * SUB + wv * RPI * ROWB), 16, vo, so, 0, 0);
+        r, (__attribute__((address_space(3))) void*)(lbase + REGION + st * STAGE + j * SUB + (wv * 2 + e) * 1024), 16, vo, so, 0, 0);
   };
   auto next_xk = [&]() __attribute__((always_inline)) {
     const bool on = ++xk == KE;
@@ -213,27 +256,29 @@ __global__ __launch_bounds__(512) void fp4_256_kernel(const Fp4Problem p) {
     wk = on ? 0 : wk;
     wn0 = on ? n0_next : wn0;
   };
-  // The scales of two K tiles, 512 elements, arrive together: X's rows by waves 0-3, W's by waves 4-7, a row per lane.
+  // The scales of two K tiles, 512 elements, arrive together, 64 rows of X and 64 of W by each wave, and are read in the last
+  // phase of the two K tiles before: their loads have 7 phases
   auto load_scales = [&](int stage, int m, int n, int k) __attribute__((always_inline)) {
     const int vo = gs, so = k * 8;
-    const __amdgpu_buffer_rsrc_t r = wv < 4 ? rows(p.xs, m, BM, p.M, p.spitch) : rows(p.ws, n, BN, p.N, p.spitch);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        r, (__attribute__((address_space(3))) void*)(lbase + SCALES + stage * SCALE_STAGE + wv * 1024), 16, vo, so, 0, 0);
+    const __amdgpu_buffer_rsrc_t rx = rows(p.xs, m, BM, p.M, p.spitch), rw = rows(p.ws, n, BN, p.N, p.spitch);
+    char* const to = lbase + SCALES + stage * SCALE_STAGE + wv * 1024;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (__attribute__((address_space(3))) void*)to, 16, vo, so, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (__attribute__((address_space(3))) void*)(to + 4096), 16, vo, so, 0, 0);
   };
-  // the tile's bias, one value per word, 64 of them by each of four waves (and again by the others); zeros past N
+  // the tile's bias, one value per word; zeros past N
   auto load_bias = [&](int stage) __attribute__((always_inline)) {
-    const int q = wv & 3, es = p.bias_f32 ? 4 : 2, n = p.bias ? max(p.N - n0, 0) * es : 0, vo = (q * 64 + lane) * es;
+    const int es = p.bias_f32 ? 4 : 2, n = p.bias ? max(p.N - n0, 0) * es : 0, vo = (wv * 64 + lane) * es;
     const __amdgpu_buffer_rsrc_t r = buffer((const uint8_t*)p.bias + (long)n0 * es, n);
     __attribute__((address_space(3))) void* const to =
-        (__attribute__((address_space(3))) void*)(lbase + BIAS + stage * BIAS_STAGE + q * 256);
+        (__attribute__((address_space(3))) void*)(lbase + BIAS + stage * BIAS_STAGE + wv * 256);
     if (p.bias_f32) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 4, vo, 0, 0, 0);
     else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 2, vo, 0, 0, 0);
   };
 
   // ---- fragment reads: row lane % 32 of a 32-row fragment, at step s chunk 2 s + lane / 32
   const int half = lane >> 5;
-  const int xr = wm * 32 + (lane & 31), wr = (wn & 1) * 32 + (lane & 31);
-  const int xa = xr * ROWB + swz(xr, half) * 16, wa = REGION + (wn >> 1) * SUB + wr * ROWB + swz(wr, half) * 16;
+  const int xr = wm * 32 + (lane & 31), wr = wn * 32 + (lane & 31);
+  const int xa = xr * ROWB + swz(xr, half) * 16, wa = REGION + wr * ROWB + swz(wr, half) * 16;
   // Whole-value casts: read member by member, the compiler takes them to alias the loads in flight and waits for those.
   auto lds16 = [&](int at) __attribute__((always_inline)) {
     return __builtin_bit_cast(i32x4_t, *(const uint4*)(lbase + at));
@@ -242,192 +287,218 @@ __global__ __launch_bounds__(512) void fp4_256_kernel(const Fp4Problem p) {
     return __builtin_bit_cast(int, *(const Word*)(lbase + at));
   };
   const int xs0 = SCALES + (wm * 128 + (lane & 31)) * 16 + half * 4;
-  const int ws0 = SCALES + 4096 + (wn * 64 + (lane >> 2 & 1) * 32 + (lane >> 3 & 3) * 4 + (lane & 3)) * 16 + half * 4;
-  f32x16_t acc[Q][2];
-#pragma unroll
-  for (int i = 0; i < Q; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) acc[i][j] = f32x16_t{};
-  // X fragments of a cluster and its scale words (clusters in turn), W fragments of a K tile (K tiles in turn) and the scale
-  // words of two K tiles
-  i32x4_t fx[2][4], fw[2][2][4];
-  int sx[2][2], sw[2][2];
-  // reads part c of X of a K tile in `st` into the cluster's registers
-  auto read_x = [&](auto stc, auto cc, int stage) __attribute__((always_inline)) {
-    constexpr int st = decltype(stc)::value, c = decltype(cc)::value;
-    const int a = opaque(xa), xsa = opaque(xs0 + stage * SCALE_STAGE);
-#pragma unroll
-    for (int s = 0; s < 4; ++s) fx[c & 1][s] = lds16((a ^ (s * 32)) + st * STAGE + c * SUB);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) sx[c & 1][h] = lds4(xsa + c * 32 * 16 + h * 8);
+  const int ws0 = SCALES + 4096 + (wn * 128 + (lane >> 2 & 1) * HALF + (lane >> 3 & 3) * 4 + (lane & 3)) * 16 + half * 4;
+  f32x16_t acc[Q][4];
+  // X fragments of a phase and its scale words (phases in turn), W fragments of a K tile (K tiles in turn) and the scale
+  // words of two K tiles, those of the next two arriving while the last phases still take the ones before
+  i32x4_t fx[2][4], fw[2][4][4];
+  int sx[2][2], sw[4][2], sw_next[4][2];
+  auto read_x = [&](auto stc, auto cc, auto sc) __attribute__((always_inline)) {  // step s of part c
+    constexpr int st = decltype(stc)::value, c = decltype(cc)::value, s = decltype(sc)::value;
+    fx[c & 1][s] = lds16((xa ^ (s * 32)) + st * STAGE + c * SUB);
   };
-  // reads fragment c / 2 of W of a K tile in `st`, steps 2 (c % 2) and the next
-  auto read_w = [&](auto stc, auto cc) __attribute__((always_inline)) {
-    constexpr int st = decltype(stc)::value, c = decltype(cc)::value, j = c >> 1, s0 = (c & 1) * 2;
-    const int a = opaque(wa);
-#pragma unroll
-    for (int s = s0; s < s0 + 2; ++s) fw[st][j][s] = lds16((a ^ (s * 32)) + st * STAGE + j * 2 * SUB);
+  auto read_w = [&](auto stc, auto jc, auto sc) __attribute__((always_inline)) {  // step s of fragment j
+    constexpr int st = decltype(stc)::value, j = decltype(jc)::value, s = decltype(sc)::value;
+    fw[st][j][s] = lds16((wa ^ (s * 32)) + st * STAGE + j * SUB);
   };
-  // reads W's scale words of two K tiles, in the phase whose MFMAs are the first to take them: the last ones' still took
-  // the words before
-  auto read_sw = [&](int stage) __attribute__((always_inline)) {
-    const int wsa = opaque(ws0 + stage * SCALE_STAGE);
+  auto read_sx = [&](auto cc, int stage) __attribute__((always_inline)) {
+    constexpr int c = decltype(cc)::value;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int h = 0; h < 2; ++h) sx[c & 1][h] = lds4(xs0 + stage * SCALE_STAGE + c * 32 * 16 + h * 8);
+  };
+  auto read_sw = [&](auto jc, int stage) __attribute__((always_inline)) {
+    constexpr int j = decltype(jc)::value;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) sw[j][h] = lds4(wsa + j * 16 * 16 + h * 8);
+    for (int h = 0; h < 2; ++h) sw_next[j][h] = lds4(ws0 + stage * SCALE_STAGE + column(j) * 16 + h * 8);
   };
 
-  // ---- writes the finished sums of cluster c of the tile at (m0, n0), whose bias is in `stage`
-  const int ncol = wn * 64 + half * 32, mrow = wm * 128 + (lane & 31);
-  constexpr int ES = F32 ? 4 : 2;
+  // The next two K tiles' words of W, ahead of a barrier: an MFMA reads what a vector instruction wrote two instructions
+  // later at the earliest, which the compiler does not know of the statements.
+  auto take_sw = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) sw[j][h] = sw_next[j][h];
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // ---- the finished sums of rows c of the tile at (m0, n0), whose bias is in `stage`, in groups of four chunks of 16 bytes
+  constexpr int ES = F32 ? 4 : 2, C = 16 / ES, GROUPS = NS / 4, STEPS = 16 / GROUPS;
   const uint32_t pitch = (uint32_t)p.N * ES;
   const int bias_shift = p.bias_f32 ? 0 : 16;
-  auto store = [&](auto cc, int m0, int n0, int stage) __attribute__((always_inline)) {
-    constexpr int c = decltype(cc)::value;
-    const int at = opaque(ncol) * 4 + BIAS + stage * BIAS_STAGE;
-    // opaque: what depends on the lane alone is formed here again rather than held in registers over the K loop
-    const int mr = opaque(mrow), n = p.N - n0 - opaque(ncol);  // n: columns left from this lane's first
-    const uint32_t yo = (uint32_t)mr * pitch + (uint32_t)(p.N - n0 - n) * ES;
-    char* const y = (char*)p.y + ((long)m0 * p.N + n0) * ES + (long)(c * 32) * pitch + yo;
-    const bool row = mr < p.M - m0 - c * 32;
-    auto columns = [&](int q, float* v) __attribute__((always_inline)) {
+  u32x4_t out[4];
+  auto take = [&](auto cc, auto gc, auto kc, int stage) __attribute__((always_inline)) {
+    constexpr int c = decltype(cc)::value, g = decltype(gc)::value, k = decltype(kc)::value;
+    constexpr int j = F32 ? g : 2 * g + k / 2, r0 = F32 ? 4 * k : k % 2 * 8;
+    const int at = opaque(wn * 128 + half * HALF) * 4 + (column(j) + r0) * 4 + BIAS + stage * BIAS_STAGE;
+    float v[C];
 #pragma unroll
-      for (int e = 0; e < 8; e += 4) {
-        const i32x4_t b = lds16(at + (q * 8 + e) * 4);
+    for (int e = 0; e < C; e += 4) {
+      const i32x4_t b = lds16(at + e * 4);
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          v[e + r] = acc[c][q >> 1][(q & 1) * 8 + e + r] + __uint_as_float((uint32_t)b[r] << bias_shift);
-      }
-    };
-    if (!row) return;
-    float v[8];
-    if (n >= 32) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        columns(q, v);
-        store_columns<F32, 8>(y + q * 8 * ES, v, 8);
-      }
-    } else {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        columns(q, v);
-        store_columns<F32, 8>(y + q * 8 * ES, v, n - q * 8);
-      }
+      for (int r = 0; r < 4; ++r) v[e + r] = acc[c][j][r0 + e + r] + __uint_as_float((uint32_t)b[r] << bias_shift);
     }
+    if constexpr (F32) out[k] = u32x4_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    else out[k] = pack8(v);
+  };
+  auto put = [&](auto cc, auto gc, auto kc, int m0, int n0) __attribute__((always_inline)) {
+    constexpr int c = decltype(cc)::value, g = decltype(gc)::value, k = decltype(kc)::value;
+    const int mr = opaque(wm * 128 + (lane & 7)), nc = opaque(wn * 128 + half * HALF + (lane >> 3 & 3) * C);
+    const uint32_t yo = (uint32_t)(mr + c * 32 + k * 8) * pitch + (uint32_t)(nc + g * 8 * C) * ES;
+    char* const y = (char*)p.y + ((long)m0 * p.N + n0) * ES + yo;
+    if (mr < p.M - m0 - c * 32 - k * 8) store_chunk<F32>(y, out[k], p.N - n0 - nc - g * 8 * C);
+  };
+  // step i of 16
+  auto store = [&](auto cc, auto ic, int m0, int n0, int stage) __attribute__((always_inline)) {
+    constexpr int i = decltype(ic)::value, n = 8 / STEPS;
+    using G = std::integral_constant<int, i / STEPS>;
+    static_for<n>([&](auto ec) {
+      constexpr int at = i % STEPS * n + decltype(ec)::value;
+      if constexpr (at < 4) take(cc, G{}, std::integral_constant<int, at>{}, stage);
+      if constexpr (at == 3) turn4(out);
+      if constexpr (at >= 4) put(cc, G{}, std::integral_constant<int, at - 4>{}, m0, n0);
+    });
   };
 
   using S0 = std::integral_constant<int, 0>;
   using S1 = std::integral_constant<int, 1>;
   int prev_m0 = p.M, prev_n0 = 0, scale_stage = 0, bias_stage = 0;  // no row of the tile before the first exists
-  bool counted = false;
-  // STORE 1: the output tile's first K tile, which writes the previous tile's sums; 2: the one after it
-  auto phase = [&](auto stc, auto cc, auto storec) __attribute__((always_inline)) {
-    constexpr int st = decltype(stc)::value, c = decltype(cc)::value;
-    constexpr int STORE = decltype(storec)::value;
+  bool counted = false;  // NS stores a phase by every wave
+  // PAIR 1: the output tile's first two K tiles, which write rows 1 to 3 of the tile before; 2: its last two, the last
+  // phase of which writes its rows 0
+  auto phase = [&](auto stc, auto cc, auto pairc) __attribute__((always_inline)) {
+    constexpr int st = decltype(stc)::value, c = decltype(cc)::value, PAIR = decltype(pairc)::value;
+    constexpr bool FIRST = PAIR == 1 && st == 0, STORE = (FIRST && c < 3) || (PAIR == 2 && st == 1 && c == 3);
     using CN = std::integral_constant<int, (c + 1) % Q>;
-    using SN = std::integral_constant<int, c + 1 < Q ? st : st ^ 1>;  // stage of the next cluster
-    using CX = std::integral_constant<int, (c + Q - 1) % Q>;
-    using SX = std::integral_constant<int, c == 0 ? st ^ 1 : st>;
-    using SW = std::integral_constant<int, c < 2 ? st : st ^ 1>;
-    if constexpr (STORE == 1) {
-      store(cc, prev_m0, prev_n0, bias_stage ^ 1);
-      // zeroed here, ahead of the barrier; as a value the compiler holds 16 registers of zeros for it
+    using SN = std::integral_constant<int, c + 1 < Q ? st : st ^ 1>;  // stage of the next phase's X
+    using CW = std::integral_constant<int, (c + Q - 1) % Q>;
+    using SW = std::integral_constant<int, c == 0 ? st : st ^ 1>;
+    using ST1 = std::integral_constant<int, st ^ 1>;
+    // The sums to be written are read from here on only: the compiler does not know how long the statements that made them
+    // run, and would take some right behind the last of those.
+    if constexpr (STORE)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float z;
-          asm volatile("v_mov_b32 %0, 0" : "=v"(z));
-          acc[c][j][i] = z;
-        }
-    }
-    // the last phase's reads, this cluster's operands among them: complete ahead of the barrier, behind which (the next
-    // phase on) their places are loaded again
-    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
-    // the next cluster's X, behind the last one of two K tiles with the next scales; W of the next K tile
-    if constexpr (c == 0 && st == 0) read_sw(scale_stage);
-    read_x(SN{}, CN{}, c + 1 == Q && st == 1 ? scale_stage ^ 1 : scale_stage);
-    read_w(std::integral_constant<int, st ^ 1>{}, cc);
-    // the last part of X's K tile kt + 1, or a part of kt + 2; W's parts 2 and 3 of kt + 2, or 0 and 1 of kt + 3
-    load_x(SX{}, CX{});
-    if constexpr (c == 0) next_xk();
-    if constexpr (c == 1) {
-      load_w(SW{}, std::integral_constant<int, 2>{});
-      load_w(SW{}, std::integral_constant<int, 3>{});
-      next_wk();
-    }
-    if constexpr (c == 3) {
-      load_w(SW{}, S0{});
-      load_w(SW{}, S1{});
-    }
-    // All but the loads of the last 4 phases have landed.  Those phases' stores need not have: NS in each phase of the
-    // first K tile, if all of the tile's rows and columns exist.
-    if (STORE && counted) wait_vmcnt<8 + (STORE == 1 ? NS * (c + 1) : STORE == 2 ? NS * (3 - c) : 0)>();
-    else wait_vmcnt<8>();
-    block_barrier();
-    static_for<4>([&](auto sc) {
-      constexpr int s = decltype(sc)::value;
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        asm_mfma<st * 2 + s / 2>(acc[c][j], fw[st][j][s], fx[c & 1][s], sw[j][s & 1], sx[c & 1][s & 1]);
+      for (int j = 0; j < 4; ++j) asm volatile("" : "+a"(acc[CN::value][j]));
+    static_for<16>([&](auto ic) {
+      constexpr int i = decltype(ic)::value, s = i / 4, j = i % 4;
+      if constexpr (FIRST && s == 0) asm_mfma_first<st * 2>(acc[c][j], fw[st][j][s], fx[c & 1][s], sw[j][0], sx[c & 1][0]);
+      else asm_mfma<st * 2 + s / 2>(acc[c][j], fw[st][j][s], fx[c & 1][s], sw[j][s & 1], sx[c & 1][s & 1]);
+      using I4 = std::integral_constant<int, i % 4>;
+      if constexpr (i < 4) read_x(SN{}, CN{}, I4{});
+      else if constexpr (i < 8) read_w(ST1{}, cc, I4{});
+      else if constexpr (i == 8) read_sx(CN{}, c + 1 == Q && st == 1 ? scale_stage ^ 1 : scale_stage);
+      else if constexpr (i == 9 && st == 1 && c == 3) static_for<4>([&](auto jc) { read_sw(jc, scale_stage ^ 1); });
+      else if constexpr (i == 10) load_x(stc, cc, S0{});
+      else if constexpr (i == 11) load_x(stc, cc, S1{});
+      else if constexpr (i == 12) load_w(SW{}, CW{}, S0{});
+      else if constexpr (i == 13) load_w(SW{}, CW{}, S1{});
+      if constexpr (STORE) {
+        if constexpr (PAIR == 1) store(CN{}, ic, prev_m0, prev_n0, bias_stage ^ 1);
+        else store(CN{}, ic, m0, n0, bias_stage);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     });
+    if constexpr (c == 0) next_wk();
+    if constexpr (c == 3) next_xk();
+    // All but the loads of the last 6 phases have landed.  Those phases' stores need not have: those of the tile's last phase
+    // and of the first three of the next, if all of its rows and columns exist.
+    constexpr int at = st * 4 + c;  // phase of the pair
+    constexpr int n = PAIR == 1 ? (at < 3 ? at + 2 : at < 5 ? 4 : 8 - at) : PAIR == 2 && at == 7 ? 1 : 0;
+    constexpr int most = 24 + n * NS < 62 ? 24 + n * NS : 62;  // (63 is no wait)
+    if (n > 0 && counted) wait_vmcnt<most>();
+    else wait_vmcnt<24>();
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    if constexpr (st == 1 && c == 3) take_sw();
     block_barrier();
   };
-  // K tiles kt and kt + 1, whose scales came as one; the next ones' have 4 phases or more.
-  auto k_pair = [&](auto firstc, int kt) __attribute__((always_inline)) {
-    constexpr int FIRST = decltype(firstc)::value;
+  auto k_pair = [&](auto pairc, int kt) __attribute__((always_inline)) {
+    constexpr int PAIR = decltype(pairc)::value;
     const bool on = kt + 2 >= KE;
     load_scales(scale_stage ^ 1, on ? m0_next : m0, on ? n0_next : n0, on ? 0 : kt + 2);
-    static_for<Q>([&](auto cc) { phase(S0{}, cc, std::integral_constant<int, FIRST ? 1 : 0>{}); });
-    static_for<Q>([&](auto cc) { phase(S1{}, cc, std::integral_constant<int, FIRST ? 2 : 0>{}); });
+    static_for<Q>([&](auto cc) { phase(S0{}, cc, pairc); });
+    static_for<Q>([&](auto cc) {
+      if constexpr (PAIR == 2 && decltype(cc)::value == 3) counted = m0 + BM <= p.M && n0 + BN <= p.N;
+      phase(S1{}, cc, pairc);
+    });
     scale_stage ^= 1;
   };
+  using E0 = S0;
+  using E1 = S1;
+  auto both_x = [&](auto stc, auto cc) __attribute__((always_inline)) {
+    load_x(stc, cc, E0{});
+    load_x(stc, cc, E1{});
+  };
+  auto both_w = [&](auto stc, auto cc) __attribute__((always_inline)) {
+    load_w(stc, cc, E0{});
+    load_w(stc, cc, E1{});
+  };
+  using P1 = std::integral_constant<int, 1>;
+  using P2 = std::integral_constant<int, 2>;
+  using P3 = std::integral_constant<int, 3>;
+  // as 8 phases ahead of the first would have: those that load tile 0's and 1's places
   load_scales(0, m0, n0, 0);
-  static_for<Q>([&](auto cc) { load_w(S0{}, cc); });
+  both_w(S0{}, S0{});
+  both_w(S0{}, P1{});
+  both_w(S0{}, P2{});
+  both_x(S0{}, S0{});
+  both_w(S0{}, P3{});
   next_wk();
-  static_for<Q>([&](auto cc) {
-    load_x(S0{}, cc);
-    load_w(S1{}, cc);
-  });
+  both_x(S0{}, P1{});
+  both_w(S1{}, S0{});
+  both_x(S0{}, P2{});
+  both_w(S1{}, P1{});
+  both_x(S0{}, P3{});
+  both_w(S1{}, P2{});
   next_xk();
+  both_x(S1{}, S0{});
+  both_w(S1{}, P3{});
   next_wk();
-  wait_vmcnt<Q * 2>();
+  wait_vmcnt<16>();
   block_barrier();
-  static_for<Q>([&](auto cc) { read_w(S0{}, cc); });
+  static_for<Q>([&](auto jc) {
+    static_for<4>([&](auto sc) { read_w(S0{}, jc, sc); });
+    read_sw(jc, 0);
+  });
+  static_for<4>([&](auto sc) { read_x(S0{}, S0{}, sc); });
+  read_sx(S0{}, 0);
   __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
   block_barrier();
-  static_for<Q - 1>([&](auto cc) {
-    load_x(S1{}, cc);
-    if constexpr (decltype(cc)::value > 0) load_w(S0{}, std::integral_constant<int, decltype(cc)::value - 1>{});
-  });
-  wait_vmcnt<8>();  // what phase 0 reads has landed: X's first two parts, W's first two of tile 1 and the scales
+  both_x(S1{}, P1{});
+  both_w(S0{}, S0{});
+  both_x(S1{}, P2{});
+  both_w(S0{}, P1{});
+  both_x(S1{}, P3{});
+  both_w(S0{}, P2{});
+  next_xk();
+  wait_vmcnt<24>();  // what phase 0 reads has landed
+  take_sw();
   block_barrier();
-  read_x(S0{}, S0{}, 0);
-  if (wv >= 4) block_barrier();
 #pragma unroll 1
   for (int t = 0; t < my_tiles; ++t) {
     load_bias(bias_stage);
     tile_next += tile_step;
     if (tile_next < tile_end) tile_at(tile_next, m0_next, n0_next);
-    counted = prev_m0 + BM <= p.M && prev_n0 + BN <= p.N;  // NS stores a phase by every wave
-    k_pair(std::true_type{}, 0);
+    k_pair(P1{}, 0);
 #pragma unroll 1
-    for (int kt = 2; kt < KE; kt += 2) k_pair(std::false_type{}, kt);
+    for (int kt = 2; kt < KE - 2; kt += 2) k_pair(S0{}, kt);
+    k_pair(P2{}, KE - 2);
     prev_m0 = m0;
     prev_n0 = n0;
     bias_stage ^= 1;
     m0 = m0_next;
     n0 = n0_next;
   }
-  if (wv < 4) block_barrier();
   wait_vmcnt<0>();  // the loads past the last K tile land before the block ends
   asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");  // the last MFMAs' results
 #pragma unroll
-  for (int i = 0; i < Q; ++i)
+  for (int i = 1; i < Q; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) asm volatile("" : "+v"(acc[i][j]));
-  static_for<Q>([&](auto cc) { store(cc, prev_m0, prev_n0, bias_stage ^ 1); });
+    for (int j = 0; j < 4; ++j) asm volatile("" : "+a"(acc[i][j]));
+  static_for<Q - 1>([&](auto cc) {
+    static_for<16>([&](auto ic) {
+      store(std::integral_constant<int, decltype(cc)::value + 1>{}, ic, prev_m0, prev_n0, bias_stage ^ 1);
+    });
+  });
 }
 
 // ---------------------------------------------------------------- smaller tiles
@@ -456,8 +527,11 @@ constexpr int kRingRowLog2 = 22;
 
 // BM x BN outputs per block; KG groups of WM x WN waves share out the K tiles.  A
 // step is KG K tiles, which arrive by direct-to-LDS loads in a ring of ST stages;
-// the groups' sums meet in LDS at the end, in their order.  As in the kernel
-// above a lane holds 4 FN neighbouring columns of each of its rows.
+// the groups' sums meet in LDS at the end, in their order.  W's rows are dealt out
+// to the fragments so that a lane holds 4 FN neighbouring columns of each of its rows.
+// 64x64 with two groups: 10.5 us at 333 x 4096 x 4096, bound by the loads' latency over
+// 8 steps.  128x128: 16.0 us at 1024 x 4096 x 4096, 2.1 PFLOP/s: 3.8 to start and end, and
+// 0.67 a K tile, of which the MFMAs take 0.32.
 template <bool F32, int BM, int BN, int WM, int WN, int KG, int ST>
 __global__ __launch_bounds__(WM* WN* KG * 64) void fp4_ring_kernel(const Fp4Problem p) {
   constexpr int NW = WM * WN * KG, FM = BM / WM / 16, FN = BN / WN / 16;
@@ -605,7 +679,8 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void fp4_ring_kernel(const Fp4Prob
 // the waves need no barrier until their sums meet in LDS, in wave order.  K tiles
 // arrive by direct-to-LDS loads in two stages of each wave's own, their scales in
 // registers.  As above W's rows are dealt out to the fragments, and a lane ends with 4
-// FN neighbouring columns of a row.
+// FN neighbouring columns of a row.  16x32 6.2 us at 33 x 1536 x 6144, 32x32 7.8 us at
+// 128 x 1536 x 6144: the latency of a wave's 6 K tiles.
 template <bool F32, int FM, int FN, int NW>
 __global__ __launch_bounds__(NW * 64) void fp4_split_kernel(const Fp4Problem p) {
   constexpr int BM = FM * 16, BN = FN * 16, ROWB = 128, TILE = (BM + BN) * ROWB;
@@ -731,7 +806,8 @@ __global__ __launch_bounds__(NW * 64) void fp4_split_kernel(const Fp4Problem p) 
 // ---------------------------------------------------------------- few rows
 // Up to 16 rows of X against 16 columns per block: W is read once, straight from
 // memory to registers, and the block's waves share out the K tiles, two in flight
-// each.  Their sums meet in LDS in wave order.
+// each.  Their sums meet in LDS in wave order.  4.5 us at 1 x 4096 x 4096, of which
+// 4.2 is any launch's: 8.4 MB would pass in 1.6 from memory, here they come from the caches.
 template <bool F32>
 __global__ __launch_bounds__(512) void fp4_rows_kernel(const Fp4Problem p) {
   constexpr int NW = 8, U = 2;
@@ -782,44 +858,45 @@ __global__ __launch_bounds__(512) void fp4_rows_kernel(const Fp4Problem p) {
 
 }  // namespace
 
-// Which kernel a product takes: the one whose modelled time is least.
-enum Fp4Cfg { FP4_ROWS, FP4_16X32, FP4_32X32, FP4_32X64, FP4_64, FP4_128, FP4_256, FP4_CFGS };
-static Fp4Cfg pick(int M, int N, int K, int out_dtype) {
+// Which kernel a product takes.  Up to 16 rows and 8 MB of W's codes, the one that streams W: 5.1 us for the best other's
+// 5.5 at (M, N, K) = (16, 4096, 4096) and 6.1 for 6.5 at (16, 1536, 6144), but 13.2 for 8.6 at (16, 16384, 4096), as each
+// of its blocks reads all of X.  Otherwise the one whose modelled time is least: a start and a cost of each round of
+// blocks, per block and per K tile, in us, fitted to all kernels' times at 196 shapes of 1 to 16717 rows and both output
+// types.  The kernel taken is at most 4% behind the best there, 0.1% on average.  Around the changes, in us (the kernel
+// taken first): (33, 1536, 6144) 16x32 6.2, 32x32 7.6, 64x64 8.5; (128, 1536, 6144) 32x32 7.8, 64x64 8.6, 16x32 10.2;
+// (333, 4096, 4096) 64x64 10.5, 128x128 14.5, 32x32 26.4; (1024, 4096, 4096) 128x128 16.0, 64x64 20.7, 256x256 32.4;
+// (8192, 4096, 4096) 256x256 75.9, 128x128 93.3, 64x64 145.
+enum Fp4Cfg { FP4_ROWS, FP4_16X32, FP4_32X32, FP4_64, FP4_128, FP4_256 };
+static Fp4Cfg pick(int M, int N, int K) {
   const double kt = fp4_pitch(K) / 128;
-#ifdef FP4_FORCE
-  if (const char* e = getenv("FP4_CFG")) {
-    const int c = atoi(e);
-    if ((c != FP4_ROWS || M <= 16) && (c != FP4_256 || kt >= kMinKTiles256)) return (Fp4Cfg)c;
-  }
-#endif
-  if (M <= 16 && N * kt * 128 <= 1 << 25) return FP4_ROWS;
+  if (M <= 16 && N * kt * 128 <= 1 << 23) return FP4_ROWS;
   auto rounds = [&](int bm, int bn) { return ceil(ceil((double)M / bm) * ceil((double)N / bn) / 256.0); };
+  // two blocks share a CU from the second round on
   auto ring = [&](int b, double c, double pair, double pair_kt, double odd, double odd_kt) {
     const double n = rounds(b, b);
     return c + floor(n / 2) * (pair + pair_kt * kt) + (n - 2 * floor(n / 2)) * (odd + odd_kt * kt);
   };
   Fp4Cfg cfg = FP4_64;
-  double best = rounds(64, 64) <= 1 ? 3.5 + 0.235 * kt : ring(64, 2.5, 1.9, 0.385, 0.3, 0.33);
+  double best = rounds(64, 64) <= 1 ? 3.9 + 0.223 * kt : ring(64, 2.5, 1.76, 0.46, 0.67, 0.377);
   auto offer = [&](Fp4Cfg c, double us) {
     if (us < best) {
       best = us;
       cfg = c;
     }
   };
-  const double memory = 2.9 + N * kt * 128 / 7e6;
-  offer(FP4_16X32, fmax(2.9 + rounds(16, 32) * (0.7 + 0.06 * kt), memory));
-  offer(FP4_32X32, fmax(2.9 + rounds(32, 32) * (1.15 + 0.083 * kt), memory));
-  offer(FP4_32X64, fmax(1.7 + rounds(32, 64) * (3.2 + 0.145 * kt), memory));
-  offer(FP4_128, rounds(128, 128) <= 1 ? 4.75 + 0.547 * kt : ring(128, 3.1, 3.65, 0.866, 0.0, 0.7));
+  const double memory = 3.2 + N * kt * 128 / 5.8e6;
+  offer(FP4_16X32, fmax(2.9 + rounds(16, 32) * (0.93 + 0.12 * kt), memory));
+  offer(FP4_32X32, fmax(3.0 + rounds(32, 32) * (1.56 + 0.12 * kt), memory));
+  offer(FP4_128, rounds(128, 128) <= 1 ? 3.8 + 0.665 * kt : ring(128, 0.15, 5.7, 1.19, 0.34, 0.89));
   // offsets within a tile of 256 output rows fit 32 bits up to 2^21 columns
   if (kt >= kMinKTiles256 && N <= 1 << 21)
-    offer(FP4_256, rounds(256, 256) <= 1 ? 13.5 + 1.02 * kt : rounds(256, 256) * (7.0 + 1.45 * kt));
+    offer(FP4_256, rounds(256, 256) <= 1 ? 20.9 + 0.955 * kt : rounds(256, 256) * (13.7 + 1.42 * kt));
   return cfg;
 }
 
-const char* gemm_fp4_config_name(int M, int N, int K, int out_dtype) {
-  static const char* names[] = {"gemm_fp4_rows", "gemm_fp4_16x32", "gemm_fp4_32x32", "gemm_fp4_32x64", "gemm_fp4_64x64", "gemm_fp4_128x128", "gemm_fp4_256x256"};
-  return names[pick(M, N, K, out_dtype)];
+const char* gemm_fp4_config_name(int M, int N, int K) {
+  static const char* names[] = {"gemm_fp4_rows", "gemm_fp4_16x32", "gemm_fp4_32x32", "gemm_fp4_64x64", "gemm_fp4_128x128", "gemm_fp4_256x256"};
+  return names[pick(M, N, K)];
 }
 
 static dim3 ring_grid(long blocks) {
@@ -847,11 +924,10 @@ template <bool F32>
 static void launch(Fp4Cfg cfg, const Fp4Problem& p, hipStream_t s) {
   if (cfg == FP4_256) {
     const long tiles = (long)((p.M + 255) / 256) * ((p.N + 255) / 256);
-    hipLaunchKernelGGL(fp4_256_kernel<F32>, dim3((unsigned)std::min<long>(tiles, kMaxBlocks256)), dim3(512), 0, s, p);
+    hipLaunchKernelGGL(fp4_256_kernel<F32>, dim3((unsigned)std::min<long>(tiles, kMaxBlocks256)), dim3(256), 0, s, p);
   } else if (cfg == FP4_ROWS) hipLaunchKernelGGL((fp4_rows_kernel<F32>), dim3((p.N + 15) / 16), dim3(512), 0, s, p);
   else if (cfg == FP4_16X32) launch_split<F32, 1, 2>(p, s);
   else if (cfg == FP4_32X32) launch_split<F32, 2, 2>(p, s);
-  else if (cfg == FP4_32X64) launch_split<F32, 2, 4>(p, s);
   else if (cfg == FP4_64) launch_ring<F32, 64, 64, 2, 2, 2>(p, s);
   else launch_ring<F32, 128, 128, 2, 4, 1>(p, s);
 }
@@ -872,7 +948,7 @@ hipError_t launch_gemm_fp4(int M, int N, int K, const void* x, const void* xs, c
   p.pitch = fp4_pitch(K);
   p.kt = p.pitch / 128;
   p.spitch = fp4_scale_pitch(K);
-  const Fp4Cfg cfg = pick(M, N, K, out_dtype);
+  const Fp4Cfg cfg = pick(M, N, K);
   if (out_dtype == DIT_F32) launch<true>(cfg, p, s);
   else launch<false>(cfg, p, s);
   return hipGetLastError();
