@@ -164,7 +164,7 @@ def test_one_token_over_a_cache(kl, heads, kv, dtype, d):
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("dtype,d", TYPES)
 @pytest.mark.parametrize("ql,kl", [([5, 64, 1, 130], [100, 64, 900, 2000]), ([0, 3, 0], [50, 0, 0]), ([10], [4]), ([200, 3], [70, 1]),
-                                   ([33, 0, 7], [5000, 10, 7]), ([600], [4000])], ids=str)
+                                   ([33, 0, 7], [5000, 10, 7]), ([600], [4000]), ([200, 1, 3, 40, 1], [9000, 5000, 100, 70, 2049])], ids=str)
 def test_parts_of_prompts_and_empty_rows(ql, kl, dtype, d, causal):
     """Queries that continue a cache, sequences without queries or keys, queries ahead of the first key."""
     c = Case(ql, kl, 6, 3, d, dtype, cache=True, seed=sum(kl))
@@ -174,6 +174,13 @@ def test_parts_of_prompts_and_empty_rows(ql, kl, dtype, d, causal):
         none = n if m == 0 else max(0, n - m) if causal else 0
         assert (o[at:at + none] == 0).all()
         at += n
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_nothing_to_do(dtype, d):
+    """Only sequences without queries: nothing is written (Case.run's guards)."""
+    Case([0, 0], [10, 0], 6, 3, d, dtype, cache=True).run(True)
+    Case([0], [3000], 6, 3, d, dtype, cache=True).run(False)
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
