@@ -75,12 +75,15 @@ __device__ __forceinline__ void asm_mfma_first(f32x16_t& c, const i32x4_t& w, co
   FP4_MFMA_BYTES("=a", "0");
 }
 
-// grouped order: 8 M-tiles share each run of N-tiles, for L2 reuse of both operands
+// grouped order: 8 M-tiles share each run of N-tiles, for L2 reuse of both operands.  Groups, which XCDs go through side by
+// side, start an eighth of the N-tiles apart: each part of W then comes from memory at its own time, most of it in the first
+// rounds, and not at the same time for all, who wait for it in every round.  16896 x 16384 x 4096 behind a kernel that
+// reads 256 MB 580 us for 668, 8192^3 277 for 290; with both operands still in the last cache the same.
 __device__ __forceinline__ void tile_of(int id, int tm, int tn, int& im, int& in) {
   constexpr int GM = 8;
   const int grp = id / (GM * tn), first = grp * GM, size = min(tm - first, GM), in_grp = id - grp * GM * tn;
   im = first + in_grp % size;
-  in = in_grp / size;
+  in = (in_grp / size + grp * max(tn / 8, 1)) % tn;
 }
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
@@ -173,7 +176,7 @@ constexpr int kMinKTiles256 = 3;    // its loads run up to three K tiles ahead, 
 // side by side; four chunks change places with those of the lanes of three other rows,
 // and a store writes 128 bytes of each of 8 rows (16 bytes of each of 64 took 1068 us
 // for 606 at 16896 x 16384 x 4096).
-// 8192^3 248 us, 4.4 PFLOP/s; 16717 x 4096 x 16384 515 us; 16896 x 16384 x 4096 571 us;
+// 8192^3 248 us, 4.4 PFLOP/s; 16717 x 4096 x 16384 525 us; 16896 x 16384 x 4096 573 us;
 // the same instructions without loads reach 6.7.  8 waves of 128 x 64, two on a SIMD, 268,
 // 555 and 667 us: they read half as much again of LDS.  Here a phase's MFMAs issue back to
 // back; its barrier, and the start and end of a block's work, take the rest.
