@@ -96,6 +96,9 @@ struct __attribute__((packed, aligned(4))) F32x4 {
 __device__ __forceinline__ u32x4_t pack8(const float* v) {
   return u32x4_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
 }
+__device__ __forceinline__ u32x4_t bits4(const float* v) {
+  return u32x4_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+}
 // C neighbouring columns (a multiple of 8) of an output row that ends `left` columns further, at any element's address
 template <bool F32, int C>
 __device__ __forceinline__ void store_columns(char* y, const float* v, int left) {
@@ -117,8 +120,8 @@ __device__ __forceinline__ void store_columns(char* y, const float* v, int left)
   }
 }
 
-// 16 bytes of an output row that ends `left` columns further, at any element's address.  Past the caches: the 256x256 tiles'
-// outputs, written line by line, would push the operands out of them (N = 16384, K = 4096: 572 us for 606).
+// 16 bytes of an output row that ends `left` columns further, at any element's address.  Past the caches, out of which the
+// outputs would push the operands: 16896 x 16384 x 4096 572 us for 606, 4429 x 1536 x 1536 11.8 for 13.0.
 template <bool F32>
 __device__ __forceinline__ void store_chunk(char* y, const u32x4_t& w, int left) {
   constexpr int C = F32 ? 4 : 8;
@@ -341,7 +344,7 @@ __global__ __launch_bounds__(256) void fp4_256_kernel(const Fp4Problem p) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) v[e + r] = acc[c][j][r0 + e + r] + __uint_as_float((uint32_t)b[r] << bias_shift);
     }
-    if constexpr (F32) out[k] = u32x4_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    if constexpr (F32) out[k] = bits4(v);
     else out[k] = pack8(v);
   };
   auto put = [&](auto cc, auto gc, auto kc, int m0, int n0) __attribute__((always_inline)) {
@@ -530,8 +533,10 @@ constexpr int kRingRowLog2 = 22;
 
 // BM x BN outputs per block; KG groups of WM x WN waves share out the K tiles.  A
 // step is KG K tiles, which arrive by direct-to-LDS loads in a ring of ST stages;
-// the groups' sums meet in LDS at the end, in their order.  W's rows are dealt out
-// to the fragments so that a lane holds 4 FN neighbouring columns of each of its rows.
+// the groups' sums meet in LDS at the end, in their order.  For bf16 outputs W's rows are
+// dealt out to the fragments so that a lane holds 8 neighbouring columns of each of its
+// rows; fp32 ones fill 64 bytes of a row by four lanes as they are (dealt out likewise,
+// and kept in the caches, 16717 x 6144 x 1536 took 165 us for 157).
 // 64x64 with two groups: 10.5 us at 333 x 4096 x 4096, bound by the loads' latency over
 // 8 steps.  128x128: 16.0 us at 1024 x 4096 x 4096, 2.1 PFLOP/s: 3.8 to start and end, and
 // 0.67 a K tile, of which the MFMAs take 0.32.
@@ -543,6 +548,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void fp4_ring_kernel(const Fp4Prob
   constexpr int TILE = (BM + BN) * ROWB, SCALES = KG * TILE, STAGE = SCALES + (BM + BN) * 16;
   static_assert(LPW * NW == UNITS && BM % 64 == 0 && BN % 64 == 0 && SU <= NW && KG <= 2, "tile config");
   static_assert(ST * STAGE <= 160 * 1024 && (KG - 1) * WM * WN * FM * FN * 1024 <= ST * STAGE, "LDS");
+  static_assert(FN == 2, "a lane's 8 columns of a row make one store of bf16, two of fp32");
   __shared__ uint4 lds[ST * STAGE / 16];
   char* const lbase = (char*)lds;
   const int tn = (p.N + BN - 1) / BN, tm = (p.M + BM - 1) / BM;
@@ -554,11 +560,11 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void fp4_ring_kernel(const Fp4Prob
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wv / (WM * WN), wm = wv / WN % WM, wn = wv % WN;
   auto swz = [](int row, int c) { return c ^ ((row >> 1) & 7); };
-  // row of X or of W that lies in row `row` of a tile: X's as they come, W's dealt out to the fragments
+  // row of X or of W that lies in row `row` of a tile: X's as they come, W's, for bf16 outputs, dealt out to the fragments
   auto source = [](int row) {
-    if (row < BM) return row;
     constexpr int C = BN / WN;
     const int w = row - BM, in_wave = w % C, f = in_wave & 15;
+    if (row < BM || F32) return row < BM ? row : w;
     return w - in_wave + (f >> 2) * (4 * FN) + (in_wave >> 4) * 4 + (f & 3);
   };
 
@@ -658,11 +664,15 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void fp4_ring_kernel(const Fp4Prob
         for (int j = 0; j < FN; ++j)
           acc[i][j] += __builtin_bit_cast(f32x4_t, part[g * WM * WN * FM * FN * 64 + (i * FN + j) * 64]);
   }
-  const int n = n0 + wn * FN * 16 + (lane >> 4) * (4 * FN);
-  if (n >= p.N) return;
+  // fragment j's four columns of a lane: 16 j from its first, so that four lanes' chunks of fp32 make 64 bytes, for bf16 4 j
+  constexpr int STEP = F32 ? 16 : 4;
+  const int n = n0 + wn * FN * 16 + (lane >> 4) * (F32 ? 4 : 4 * FN);
   float b[4 * FN];
 #pragma unroll
-  for (int i = 0; i < 4 * FN; ++i) b[i] = n + i < p.N ? bias_at(p, n + i) : 0.f;
+  for (int i = 0; i < 4 * FN; ++i) {
+    const int at = n + i / 4 * STEP + i % 4;
+    b[i] = at < p.N ? bias_at(p, at) : 0.f;
+  }
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
     const long m = m0 + wm * FM * 16 + i * 16 + (lane & 15);
@@ -672,7 +682,13 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void fp4_ring_kernel(const Fp4Prob
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) v[j * 4 + r] = acc[i][j][r] + b[j * 4 + r];
-    store_columns<F32, 4 * FN>((char*)p.y + (m * p.N + n) * (F32 ? 4 : 2), v, p.N - n);
+    char* const y = (char*)p.y + (m * p.N + n) * (F32 ? 4 : 2);
+    if constexpr (F32) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) store_chunk<F32>(y + j * STEP * 4, bits4(v + j * 4), p.N - n - j * STEP);
+    } else {
+      store_chunk<F32>(y, pack8(v), p.N - n);
+    }
   }
 }
 
@@ -862,13 +878,14 @@ __global__ __launch_bounds__(512) void fp4_rows_kernel(const Fp4Problem p) {
 }  // namespace
 
 // Which kernel a product takes.  Up to 16 rows and 8 MB of W's codes, the one that streams W: 5.1 us for the best other's
-// 5.5 at (M, N, K) = (16, 4096, 4096) and 6.1 for 6.5 at (16, 1536, 6144), but 13.2 for 8.6 at (16, 16384, 4096), as each
+// 5.3 at (M, N, K) = (16, 4096, 4096) and 6.1 for 6.3 at (16, 1536, 6144), but 13.2 for 8.6 at (16, 16384, 4096), as each
 // of its blocks reads all of X.  Otherwise the one whose modelled time is least: a start and a cost of each round of
 // blocks, per block and per K tile, in us, fitted to all kernels' times at 196 shapes of 1 to 16717 rows and both output
-// types.  The kernel taken is at most 4% behind the best there, 0.1% on average.  Around the changes, in us (the kernel
-// taken first): (33, 1536, 6144) 16x32 6.2, 32x32 7.6, 64x64 8.5; (128, 1536, 6144) 32x32 7.8, 64x64 8.6, 16x32 10.2;
-// (333, 4096, 4096) 64x64 10.5, 128x128 14.5, 32x32 26.4; (1024, 4096, 4096) 128x128 16.0, 64x64 20.7, 256x256 32.4;
-// (8192, 4096, 4096) 256x256 75.9, 128x128 93.3, 64x64 145.
+// types.  The kernel taken is 0.2% behind the best there on average, and at most 1% but for up to 15% at three shapes of 700
+// columns in fp32, where 64x64 tiles are better than their rounds.  Around the changes, in us (the kernel
+// taken first): (33, 1536, 6144) 16x32 6.3, 32x32 7.7, 64x64 8.6; (128, 1536, 6144) 32x32 7.8, 64x64 8.7, 16x32 10.3;
+// (333, 4096, 4096) 64x64 10.4, 128x128 14.7, 32x32 26.5; (1024, 4096, 4096) 128x128 16.2, 64x64 20.9, 256x256 32.6;
+// (8192, 4096, 4096) 256x256 79, 128x128 99, 64x64 150.
 enum Fp4Cfg { FP4_ROWS, FP4_16X32, FP4_32X32, FP4_64, FP4_128, FP4_256 };
 static Fp4Cfg pick(int M, int N, int K) {
   const double kt = fp4_pitch(K) / 128;
@@ -880,20 +897,20 @@ static Fp4Cfg pick(int M, int N, int K) {
     return c + floor(n / 2) * (pair + pair_kt * kt) + (n - 2 * floor(n / 2)) * (odd + odd_kt * kt);
   };
   Fp4Cfg cfg = FP4_64;
-  double best = rounds(64, 64) <= 1 ? 3.9 + 0.223 * kt : ring(64, 2.5, 1.76, 0.46, 0.67, 0.377);
+  double best = rounds(64, 64) <= 1 ? 4.0 + 0.22 * kt : ring(64, 2.0, 1.76, 0.475, 0.0, 0.408);
   auto offer = [&](Fp4Cfg c, double us) {
     if (us < best) {
       best = us;
       cfg = c;
     }
   };
-  const double memory = 3.2 + N * kt * 128 / 5.8e6;
-  offer(FP4_16X32, fmax(2.9 + rounds(16, 32) * (0.93 + 0.12 * kt), memory));
-  offer(FP4_32X32, fmax(3.0 + rounds(32, 32) * (1.56 + 0.12 * kt), memory));
-  offer(FP4_128, rounds(128, 128) <= 1 ? 3.8 + 0.665 * kt : ring(128, 0.15, 5.7, 1.19, 0.34, 0.89));
+  const double memory = 3.3 + N * kt * 128 / 5.6e6;
+  offer(FP4_16X32, fmax(3.0 + rounds(16, 32) * (0.94 + 0.12 * kt), memory));
+  offer(FP4_32X32, fmax(3.2 + rounds(32, 32) * (1.18 + 0.144 * kt), memory));
+  offer(FP4_128, rounds(128, 128) <= 1 ? 4.26 + 0.635 * kt : ring(128, 0.44, 5.7, 1.19, 0.74, 0.89));
   // offsets within a tile of 256 output rows fit 32 bits up to 2^21 columns
   if (kt >= kMinKTiles256 && N <= 1 << 21)
-    offer(FP4_256, rounds(256, 256) <= 1 ? 20.9 + 0.955 * kt : rounds(256, 256) * (13.7 + 1.42 * kt));
+    offer(FP4_256, rounds(256, 256) <= 1 ? 21.4 + 0.95 * kt : rounds(256, 256) * (13.7 + 1.47 * kt));
   return cfg;
 }
 
