@@ -538,7 +538,7 @@ __global__ __launch_bounds__(256) void grouped_f32_kernel(const GroupedArgs a) {
 // the softmax runs; its V likewise, the next one's arriving beside the next scores.  So
 // one place each is enough, two blocks share a CU, and what a CU has in flight is what
 // its LDS holds.  The reads of K and V bound it, each once: sixteen sequences of 1 to
-// 16384 keys, 8 key heads of 128, 258 MB, 58 us with the joining of the ranges, 4.5 TB/s
+// 16384 keys, 8 key heads of 128, 258 MB, 54 us with the joining of the ranges, 4.8 TB/s
 // (334 us by the kernel of many rows, whole sequences; 84 in ranges of 512 keys).
 constexpr int kFewRows = 32, kFewKeys = 32, kFewWaves = 4;
 constexpr int kStreamed = 2;  // a load's cache policy: not to be kept (58 us; kept 62)
@@ -791,8 +791,8 @@ void grouped_few_kernel(const GroupedArgs a) {
 
 // ---------------------------------------------------------------- ranges of keys joined
 // A row's ranges in their order; `t` of the HD / 4 threads that take 4 dimensions each.  FEW: tiles of kFewRows rows, one to
-// a sequence, whose ranges may be many: a block takes one row, and its 8 groups of threads every 8th range each, which meet
-// in LDS.  Otherwise the block of a tile's first range takes the tile, 8 rows at a time.
+// a sequence, whose ranges may be many: a block takes one row (`rows` to a sequence, what the longest has: kFewRows cost 3 of
+// 57 us where each has four), and its 8 groups of threads every 8th range each, which meet in LDS.  Otherwise the block of a tile's first range takes the tile, 8 rows at a time.
 struct Joined {
   float m, l;
   float4 y;
@@ -813,16 +813,16 @@ __device__ __forceinline__ Joined join_ranges(const float2* ml, const float* po,
 }
 
 template <typename T, int HD, bool FEW>
-__global__ __launch_bounds__(HD * 2) void grouped_merge_kernel(const GroupedArgs a, int per) {
+__global__ __launch_bounds__(HD * 2) void grouped_merge_kernel(const GroupedArgs a, int per, int rows) {
   constexpr int TPR = HD / 4, GROUPS = 8;
   __shared__ float4 part_y[FEW ? GROUPS : 1][TPR];
   __shared__ float2 part_m[FEW ? GROUPS : 1];
   int id = block_id();
   const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
   if constexpr (FEW) {
-    const int s = id / (a.kv_heads * kFewRows), h = id / kFewRows % a.kv_heads;
+    const int s = id / (a.kv_heads * rows), h = id / rows % a.kv_heads;
     if (s >= a.n_seq) return;
-    const int row = id % kFewRows;
+    const int row = id % rows;
     id = a.tile_off[s] * a.kv_heads + h;
     const Unit u = unit_of(a, id, per);
     if (u.ranges == 1 || row >= u.rows) return;
@@ -921,9 +921,11 @@ Plan plan_of(const GroupedArgs& in, Kind kind, bool may_cut = true) {
 template <typename T, bool FEW_ROWS>
 void launch_merge(const Plan& p, hipStream_t s) {
   if (p.bytes == 0) return;
-  const dim3 grid = grid_of(FEW_ROWS ? (long)p.a.n_seq * p.a.kv_heads * kFewRows : p.units);
-  if (p.a.head_dim == 64) hipLaunchKernelGGL((grouped_merge_kernel<T, 64, FEW_ROWS>), grid, dim3(128), 0, s, p.a, p.per);
-  else hipLaunchKernelGGL((grouped_merge_kernel<T, 128, FEW_ROWS>), grid, dim3(256), 0, s, p.a, p.per);
+  int rows = 0;  // of the sequence with most
+  for (int i = 0; i < p.a.n_seq; ++i) rows = std::max(rows, p.a.q_len[i] * p.a.group);
+  const dim3 grid = grid_of(FEW_ROWS ? (long)p.a.n_seq * p.a.kv_heads * rows : p.units);
+  if (p.a.head_dim == 64) hipLaunchKernelGGL((grouped_merge_kernel<T, 64, FEW_ROWS>), grid, dim3(128), 0, s, p.a, p.per, rows);
+  else hipLaunchKernelGGL((grouped_merge_kernel<T, 128, FEW_ROWS>), grid, dim3(256), 0, s, p.a, p.per, rows);
 }
 
 }  // namespace
