@@ -418,10 +418,10 @@ dit_status dit_rope_frequencies(int rot_dim, double theta, double factor, double
  * from one row to the next, at least heads * head_dim, so the query and key heads
  * of a fused product's rows turn in one call.  positions: int32 device array
  * [rows], any values; NULL: row r is at position r.  w: host array of rot_dim / 2
- * frequencies (any finite values), read during the call.  Angles are formed in 64
+ * frequencies (of at most 2^64 in magnitude), read during the call.  Angles are formed in 64
  * bits, the rotation in fp32, rounded once to dtype.  y may be x itself with ldy =
  * ldx; otherwise they may not overlap.  x, y aligned to their elements; rows >= 0,
- * head_dim <= 1024, rot_dim <= head_dim.
+ * heads <= 2^16, head_dim <= 1024, rot_dim <= head_dim.
  */
 #define DIT_ROPE_HALF 0
 #define DIT_ROPE_PAIRS 1
@@ -434,7 +434,9 @@ dit_status dit_rope(int rows, int heads, int head_dim, int rot_dim, int layout, 
  * keys and q_len[s] >= 0 queries.  Its queries follow those of the sequences
  * before it; its keys are the rows kv_row[s], kv_row[s] + 1, .. of k and v (slots
  * of a cache, or rows that several sequences share), or with kv_row NULL follow the
- * keys of the sequences before it.
+ * keys of the sequences before it.  At most 2^24 queries in all, 2^24 keys to a
+ * sequence and 2^30 for its queries times the heads that share a key head;
+ * kv_row[s] <= 2^40.
  */
 #define DIT_MAX_SEQUENCES 128
 typedef struct {

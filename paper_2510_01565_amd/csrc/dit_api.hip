@@ -732,6 +732,7 @@ dit_status check_fp4_shape(int rows, int K) {
 }
 
 constexpr int kMaxText = 1 << 24;  // queries, or keys of one sequence
+constexpr int kMaxRows = 1 << 30;  // queries of a sequence times heads to a key head
 constexpr int kMaxRow = 1 << 22;   // elements between rows: offsets within a tile of 64 keys fit 32 bits
 
 // Checks the sequences and heads, and lays the sequences out longest first: their tiles are numbered in that order,
@@ -768,6 +769,8 @@ dit_status check_grouped(const dit_sequences* q, int heads, int kv_heads, int he
     queries += q->q_len[s];
     keys += q->kv_len[s];
     if (queries > kMaxText) return fail(DIT_ERR_UNSUPPORTED, "more than %d queries", kMaxText);
+    if ((long)q->q_len[s] * a->group > kMaxRows)
+      return fail(DIT_ERR_UNSUPPORTED, "sequence %d: q_len %d of %d heads to a key head", s, q->q_len[s], a->group);
   }
   std::stable_sort(order, order + q->n_seq, [&](int x, int y) { return q->kv_len[x] > q->kv_len[y]; });
   for (int i = 0; i < q->n_seq; ++i) {
@@ -1349,7 +1352,7 @@ dit_status dit_rope(int rows, int heads, int head_dim, int rot_dim, int layout, 
   if (dtype != DIT_F32 && dtype != DIT_BF16) return fail(DIT_ERR_INVALID_ARG, "dtype %d", dtype);
   if (!w) return fail(DIT_ERR_INVALID_ARG, "w is NULL");
   for (int i = 0; i < rot_dim / 2; ++i)
-    if (!isfinite(w[i])) return fail(DIT_ERR_INVALID_ARG, "w[%d] is not finite", i);
+    if (!(fabs(w[i]) <= 0x1p64)) return fail(DIT_ERR_INVALID_ARG, "w[%d] = %g is not within 2^64", i, w[i]);  // or an angle overflows
   if (!isfinite(magnitude)) return fail(DIT_ERR_INVALID_ARG, "magnitude is not finite");
   const long width = (long)heads * head_dim;
   if (ldx < width || ldy < width) return fail(DIT_ERR_INVALID_ARG, "ldx %ld or ldy %ld below heads * head_dim = %ld", ldx, ldy, width);

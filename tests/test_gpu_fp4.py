@@ -3,6 +3,8 @@
 Tolerances.  Codes, scales and values: equal.  fp32 output: of each 8 products, which share their scales, the sum is
 exact; every addition of such a sum loses less than one step of fp32 (2^-23, whether it rounds or cuts) of the products'
 magnitudes, and the bias one more: (K / 8 + 2) 2^-23 of them.  bf16 output: half a step (2^-8 of the value) more."""
+import math
+
 import numpy as np
 import pytest
 
@@ -256,6 +258,29 @@ def test_linear_fp4_large(M, N, K, out):
 @pytest.mark.parametrize("M,N,K,off", [(3, 77, 200, 1), (90, 333, 300, 1), (2100, 2047, 900, 3), (4096, 4096, 1024, 1), (8190, 8190, 700, 3)])
 def test_output_anywhere_its_elements_may_lie(M, N, K, off, out):
     _large(M, N, K, out, True, 11, off)
+
+
+@pytest.mark.parametrize("bias", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [(3, 77, 200), (40, 333, 1500), (200, 333, 300), (1030, 2050, 390), (3500, 3490, 1700)])
+def test_bias_anywhere_its_elements_may_lie(M, N, K, bias):
+    """A bias one element behind a 16-byte boundary gives the same bits as one at it."""
+    torch = _torch()
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    ops = []
+    for rows in (M, N):
+        t = torch.randn((rows, K), generator=gen, device="cuda")
+        nc, ns = dit.fp4_layout(rows, K)
+        ops += [torch.empty(nc, dtype=torch.uint8, device="cuda"), torch.empty(ns, dtype=torch.uint8, device="cuda")]
+        dit.dit_quantize_fp4(rows, K, dit.DIT_F32, t, ops[-2], ops[-1])
+    b = torch.randn(N, generator=gen, device="cuda").to(_dt(bias)[0])
+    shifted = torch.cat([torch.full((1,), math.nan, device="cuda", dtype=b.dtype), b, torch.full((9,), math.nan, device="cuda", dtype=b.dtype)])
+    outs = []
+    for v in (b, shifted[1:], None):
+        y = torch.empty((M, N), dtype=torch.float32, device="cuda")
+        dit.dit_linear_fp4(M, N, K, *ops, v, _dt(bias)[1], y, dit.DIT_F32)
+        outs.append(y)
+    assert torch.equal(outs[0], outs[1])
+    assert torch.isfinite(outs[0]).all() and torch.equal(outs[2] + b.float(), outs[0])
 
 
 def test_one_long_row_and_one_long_column():

@@ -101,6 +101,7 @@ def test_rope_refusals():
     assert _err(dit.dit_rope, 5, 1, 512, 258, 0, BF, P, [0.1] * 129, 1.0, P, 512, P, 512, 0) == UNS
     assert bad((4, 2)) == BAD and bad((5, 3)) == BAD and bad((7, None)) == BAD
     assert bad((7, [0.1] * 15 + [INF])) == BAD and bad((7, [NAN] * 16)) == BAD and bad((8, NAN)) == BAD and bad((8, INF)) == BAD
+    assert bad((7, [0.1] * 15 + [1e300])) == BAD and bad((7, [-2.0 ** 65] + [0.1] * 15)) == BAD  # angles past a double's range
     assert bad((10, 191)) == BAD and bad((12, 191)) == BAD
     assert bad((9, 0)) == BAD and bad((11, 0)) == BAD and bad((9, P + 1)) == BAD and bad((11, P + 1)) == BAD and bad((6, P + 2)) == BAD
     assert bad((12, 200)) == BAD  # in place with another stride
@@ -132,6 +133,10 @@ def test_grouped_refusals():
     for fn in (lambda *c: bad(*c), lambda *c: _refusals(size, ok[:5])(*c)):
         assert fn((1, 0)) == BAD and fn((2, 0)) == BAD and fn((2, 4)) == BAD and fn((1, 1026), (2, 1)) == UNS
         assert fn((3, 96)) == UNS and fn((4, 2)) == BAD and fn((3, 128), (4, F32)) == UNS
+    # 2^21 queries of 1024 heads to one key head
+    many = dit.Sequences([1 << 21], [1])
+    assert _err(size, many, 1024, 1, 64, BF) == UNS and size(many, 1024, 1024, 64, BF) >= 0
+    assert _err(dit.dit_attention_grouped, many, 1024, 1, 64, BF, 0, 0.125, P, 65536, P, P, 64, P, 65536, P, 1 << 40, 0) == UNS
     assert bad((5, 2)) == BAD and all(bad((6, v)) == BAD for v in (NAN, INF, 0.0, -1.0, 1e-20, 1e20))
     for i in (7, 9, 10, 12):
         assert bad((i, 0)) == BAD and bad((i, P + 8)) == BAD
