@@ -358,7 +358,8 @@ dit_status dit_attention_sparse(const dit_batch* batch, int heads, int head_dim,
  *  - scales: one byte each, s = 2^(byte - 127), 255 = NaN, [rows][16 ceil(K / 512)]:
  *    block 4 i + j of a row's 16 blocks of 512 elements is byte 4 j + i of their
  *    16 (the order in which the matrix cores take them), 127 past the last block.
- * dit_fp4_layout returns the bytes of both buffers.  rows >= 0, 1 <= K <= 2^22.
+ * dit_fp4_layout returns the bytes of both buffers.  rows >= 0, 1 <= K <= 2^22,
+ * rows ceil(K / 512) <= 2^31.
  */
 #define DIT_FP4_BLOCK 32
 dit_status dit_fp4_layout(int rows, int K, size_t* code_bytes, size_t* scale_bytes);

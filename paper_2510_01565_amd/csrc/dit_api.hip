@@ -728,6 +728,8 @@ SparseMeta make_sparse_meta(const dit_batch* b) {
 dit_status check_fp4_shape(int rows, int K) {
   if (rows < 0 || K <= 0) return fail(DIT_ERR_INVALID_ARG, "rows %d K %d", rows, K);
   if (K > kFp8MaxK) return fail(DIT_ERR_UNSUPPORTED, "K %d exceeds %d", K, kFp8MaxK);
+  if ((long)rows * (fp4_scale_pitch(K) / 16) > 1L << 31)
+    return fail(DIT_ERR_UNSUPPORTED, "rows %d x ceil(K %d / 512) exceeds 2^31", rows, K);
   return DIT_OK;
 }
 

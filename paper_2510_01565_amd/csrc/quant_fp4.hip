@@ -54,14 +54,14 @@ __device__ __forceinline__ void load8(const T* x, int n, float* v) {
   }
 }
 
-// The row and the chunk of 512 elements of unit `unit`, the same for a wave's lanes; a 64-bit division only where it is needed
+// a wave's row and chunk of 512 elements, of at most 2^31 in all
 struct Chunk {
   long unit, row;
   int c;
 };
 __device__ __forceinline__ Chunk chunk_of(long rows, int chunks) {
   const long unit = (long)block_id() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long row = rows * chunks >> 32 ? unit / chunks : (uint32_t)unit / (uint32_t)chunks;
+  const long row = (uint32_t)unit / (uint32_t)chunks;
   return {unit, row, (int)(unit - row * chunks)};
 }
 

@@ -38,6 +38,7 @@ def test_fp4_shapes_are_checked():
     assert _err(dit.fp4_layout, -1, 8) == BAD
     assert _err(dit.fp4_layout, 1, 0) == BAD
     assert _err(dit.fp4_layout, 1, (1 << 22) + 1) == UNS
+    assert _err(dit.fp4_layout, (1 << 18) + 1, 1 << 22) == UNS and dit.fp4_layout(1 << 18, 1 << 22) == (1 << 39, 1 << 35)
 
 
 def test_quantize_fp4_refusals():
