@@ -408,3 +408,55 @@ def test_an_encoder_layer_and_one_token_more():
     a, b = ot.double(), o[new].double()
     # either is within the attention's own bound of the same values; the rows they read agree to a rounding
     assert float((a - b).norm() / b.norm()) < 2.0 ** -6
+
+
+def test_two_layers_at_once_on_two_streams():
+    """Quantise, product, rotary positions in place and attention, once after the other, then side by side on streams of
+    their own with buffers of their own: the same bits."""
+    torch = _torch()
+    heads, kv, d, K = 24, 8, 64, 8192
+    W = (heads + 2 * kv) * d
+    gen = torch.Generator(device="cuda").manual_seed(21)
+    rnd = lambda std, *s: (std * torch.randn(s, generator=gen, device="cuda")).to(torch.bfloat16)
+    w = dit.rope_frequencies(d, 10000.0)
+    wq, ws = _fp4(rnd(K ** -0.5, W, K))
+
+    class Layer:
+        def __init__(self, ql, kl):
+            self.rows = sum(ql)
+            self.x, self.qs = rnd(1.0, self.rows, K), dit.fp4_layout(self.rows, K)
+            self.codes, self.scales = (torch.empty(n, dtype=torch.uint8, device="cuda") for n in self.qs)
+            self.y = torch.empty((self.rows, W), dtype=torch.bfloat16, device="cuda")
+            self.o = torch.empty((self.rows, heads * d), dtype=torch.bfloat16, device="cuda")
+            self.seqs = dit.Sequences(ql, kl, None if ql == kl else [0] * len(ql))
+            self.cache = None if ql == kl else rnd(1.0, max(kl), 2 * kv * d)
+            self.n = dit.attention_grouped_workspace_size(self.seqs, heads, kv, d, dit.DIT_BF16)
+            self.ws = torch.empty(max(self.n, 256), dtype=torch.uint8, device="cuda")
+
+        def run(self):
+            dit.dit_quantize_fp4(self.rows, K, dit.DIT_BF16, self.x, self.codes, self.scales)
+            dit.dit_linear_fp4(self.rows, W, K, self.codes, self.scales, wq, ws, None, dit.DIT_BF16, self.y, dit.DIT_BF16)
+            dit.dit_rope(self.rows, heads + kv, d, d, dit.DIT_ROPE_HALF, dit.DIT_BF16, None, w, 1.0, self.y, W, self.y, W)
+            k, v, ld = ((self.y[:, heads * d:], self.y[:, (heads + kv) * d:], W) if self.cache is None
+                        else (self.cache, self.cache[:, kv * d:], 2 * kv * d))
+            dit.dit_attention_grouped(self.seqs, heads, kv, d, dit.DIT_BF16, dit.DIT_CAUSAL, 0.125, self.y, W, k, v, ld, self.o,
+                                      heads * d, self.ws, self.n)
+
+    layers = [Layer([4096, 204], [4096, 204]), Layer([1] * 40, [9000] * 20 + [333] * 20), Layer([2000, 1], [2000, 1])]
+    want = []
+    for layer in layers:
+        layer.run()
+        want.append(layer.o.clone())
+        assert torch.isfinite(layer.o).all()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in layers]
+    for _ in range(3):
+        for layer in layers:
+            layer.o.zero_()
+        torch.cuda.synchronize()
+        for layer, s in zip(layers, streams):
+            with torch.cuda.stream(s):
+                layer.run()
+        torch.cuda.synchronize()
+        for layer, r in zip(layers, want):
+            assert torch.equal(layer.o, r)
