@@ -158,6 +158,7 @@ __device__ __forceinline__ void turn4(u32x4_t (&w)[4]) {
 
 // ---------------------------------------------------------------- 256 x 256 tiles
 constexpr int kMaxBlocks256 = 256;  // one per CU
+constexpr int kStaggerKTiles = 8, kStaggerRounds = 6;
 constexpr int kMinKTiles256 = 3;    // its loads run up to three K tiles ahead, into the next output tile at most
 
 // 4 waves, one per SIMD, each 128 rows x 128 columns by 32x32x64 matrix instructions: 16
@@ -441,6 +442,11 @@ __global__ __launch_bounds__(256) void fp4_256_kernel(const Fp4Problem p) {
   using P1 = std::integral_constant<int, 1>;
   using P2 = std::integral_constant<int, 2>;
   using P3 = std::integral_constant<int, 3>;
+  // Blocks that finish a tile at the same time write at the same time, and wait for it.  An XCD's 32 blocks start up to 6 us
+  // apart where a block has several tiles of short K to win that back: behind the quantising of X 16896 x 8192 x 2048 takes
+  // 196 us for 206, 16896 x 16384 x 1024 242 for 256, 16717 x 6144 x 1536 135 for 136; but 16896 x 16384 x 4096 617 for 609.
+  if (KT <= kStaggerKTiles && tiles >= kStaggerRounds * kMaxBlocks256)
+    for (int i = (int)blockIdx.x >> 3; i > 0; --i) __builtin_amdgcn_s_sleep(6);
   // as 8 phases ahead of the first would have: those that load tile 0's and 1's places
   load_scales(0, m0, n0, 0);
   both_w(S0{}, S0{});

@@ -249,7 +249,7 @@ def _large(M, N, K, out, bias, seed, off=0):
 
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 @pytest.mark.parametrize("M,N,K", [(16, 16384, 4096), (1, 20011, 4100), (100, 4096, 4096), (700, 3333, 2000), (4429, 1536, 1536),
-                                   (2049, 2303, 777), (3500, 3490, 1700), (9000, 4500, 2000), (8190, 8190, 700), (5000, 6144, 1536), (4100, 8190, 1280), (8192, 4096, 512), (3000, 3000, 64)])
+                                   (2049, 2303, 777), (3500, 3490, 1700), (9000, 4500, 2000), (16717, 6150, 2000), (8190, 8190, 700), (5000, 6144, 1536), (4100, 8190, 1280), (8192, 4096, 512), (3000, 3000, 64)])
 def test_linear_fp4_large(M, N, K, out):
     _large(M, N, K, out, (M + K) % 2 == 0, M + N)
 

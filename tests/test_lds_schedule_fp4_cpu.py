@@ -9,6 +9,7 @@ from test_lds_schedule_cpu import CLANG, CSRC, MAIN, RUNTIME, _counts, needs_cla
 
 RUNTIME4 = RUNTIME + r"""
 #define __builtin_amdgcn_raw_buffer_load_b32 trace::load_b8
+#define __builtin_amdgcn_s_sleep(x)
 struct Two { uint32_t v[2]; uint32_t operator[](int i) const { return v[i]; } };
 #define __builtin_amdgcn_permlane16_swap(a, b, ...) (Two{{a, b}})
 #define __builtin_amdgcn_update_dpp(a, b, ...) (b)
