@@ -883,7 +883,9 @@ Plan plan_of(const GroupedArgs& in, Kind kind, bool may_cut = true) {
   p.a = in;
   GroupedArgs& a = p.a;
   p.per = kind == F32 ? FQ : kind == FEW ? kFewRows : 128;
-  // sequences of few rows have a kernel of their own, unless they are short and the other one is launched anyway
+  // Sequences of few rows have a kernel of their own, unless they are short and the other one is launched anyway: three
+  // prompts of 1024 tokens with eight tokens over 500 keys each 26 us in one launch, 34 in two, over 2048 34 and 40, over
+  // 4096 44 and 45 (the tokens alone 334 and 54 for sixteen of up to 16384).
   bool many = false;
   for (int i = 0; i < in.n_seq; ++i) many = many || (long)in.q_len[i] * in.group > kFewRows;
   a.n_seq = 0;
@@ -896,7 +898,10 @@ Plan plan_of(const GroupedArgs& in, Kind kind, bool may_cut = true) {
     a.kv_row[a.n_seq] = in.kv_row[i];
     ++a.n_seq;
   }
-  // Ranges as long as what one of 512 blocks (two to a CU) takes if all take the same.
+  // Ranges as long as what one of 512 blocks (two to a CU) takes if all take the same, of 256 with many rows, and not below
+  // `least`, as joining them takes another launch.  Whole, and in ranges: few rows, four sequences of 512 keys 8.8 us and
+  // 12.1, of 1024 15.8 and 13.2; many rows, 300 queries over 2048 keys 39 and 47, 64 over 4096 67 and 43 (in ranges of 2048
+  // keys 60, of 512 46).  One token over 4096 keys 13.5 in ranges of 256, 14.4 of 64.
   constexpr int kWhole = 1 << 30;
   double keys = 0;
   int longest = 0;
@@ -904,8 +909,12 @@ Plan plan_of(const GroupedArgs& in, Kind kind, bool may_cut = true) {
     keys += (double)(((long)a.q_len[i] * a.group + p.per - 1) / p.per) * a.kv_heads * a.kv_len[i];
     longest = std::max(longest, a.kv_len[i]);
   }
-  const double even = fmax(keys / 512 * (kind == ROWS ? 2 : 1), kind == ROWS ? 2048 : 256);
-  a.chunk = !may_cut || longest <= 768 || even >= longest ? kWhole : ((int)even + kKeys - 1) / kKeys * kKeys;
+  const int least = kind == ROWS ? 1024 : 256, whole = kind == ROWS ? 2048 : 768;
+  double even = fmax(keys / 512 * (kind == ROWS ? 2 : 1), least);
+  // Many rows: no more than 256 blocks in the end (300 queries over 4096 keys 62 us, one range more to a tile 72), and no more
+  // than 8 ranges of a tile, which one block joins (64 over 16384 69 us, 16 ranges 76, 4 ranges 87).
+  if (kind == ROWS) even = fmax(longest / fmin(fmax(floor(longest / even), 1.0), 8.0), least);
+  a.chunk = !may_cut || longest <= whole || even >= longest ? kWhole : ((int)even + kKeys - 1) / kKeys * kKeys;
   a.tile_off[0] = 0;
   bool cut = false;
   for (int i = 0; i < a.n_seq; ++i) {
