@@ -4,9 +4,10 @@
 // The angle is formed in 64 bits, in turns: pos * (w / 2 pi), of which the nearest
 // whole number is taken off; what is left goes to fp32 and to sine and cosine of a
 // multiple of pi.  A block forms the sines and cosines of its tokens' pairs once, in
-// LDS, for all heads.  Memory bounds it: x is read once and y written once, both past
-// the caches (66 us with them): 62 us at 16391 tokens of 40 heads of 128, 5.4 TB/s, as
-// fast as a copy.  A single token takes 5.7 us, of which 4.2 is any launch's.
+// LDS, for all heads, while its first pieces are on their way.  Memory bounds it: x is
+// read once and y written once, both past the caches: 56 us at 16391 tokens of 40 heads
+// of 128, half of each turned, 6.0 TB/s; 62 with the loads behind the sines, 66 through
+// the caches.  A single token takes 5.7 us, of which 4.2 is any launch's.
 #include <math.h>
 
 #include "device_common.h"
@@ -63,42 +64,33 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
   const long row = block_id();
   if (row >= a.rows) return;
   const int pairs = a.rot / 2;
-  const int pos = a.pos ? a.pos[row] : (int)row;
-  for (int i = threadIdx.x; i < pairs; i += 256) {
-    double t = (double)pos * a.turns[i];
-    t -= rint(t);
-    float s, c;
-    sincospif(2.0f * (float)t, &s, &c);
-    cs[i] = make_float2(c * a.magnitude, s * a.magnitude);
-  }
-  __syncthreads();
   const T* const x = (const T*)a.x + row * a.ldx;
   T* const y = (T*)a.y + row * a.ldy;
   constexpr int E = WIDE ? 16 / sizeof(T) : 1;  // elements of a piece
+  constexpr int P = HALF ? E : WIDE ? E : 2;    // of what is loaded at once
   // a head's work: pieces of the turned part (of its first half, HALF), then pieces that are copied
   const int turned = HALF ? pairs / E : (WIDE ? a.rot / E : pairs), copied = x == y ? 0 : (a.d - a.rot) / E;
-  const int per = turned + copied;
-  for (int u = threadIdx.x; u < a.heads * per; u += 256) {
-    const int h = u / per, c = u - h * per, at = h * a.d;
+  const int per = turned + copied, units = a.heads * per;
+  float p[P], q[P];
+  int c, e;
+  auto load = [&](int u) __attribute__((always_inline)) {
+    const int h = u / per;
+    c = u - h * per;
+    e = h * a.d + (c >= turned ? a.rot + (c - turned) * E : c * P);
+    if constexpr (WIDE) {
+      load16b(x + e, p);
+      if constexpr (HALF)
+        if (c < turned) load16b(x + e + pairs, q);
+    } else {
+      p[0] = to_f32<T>(x[e]);
+      if (c < turned) (HALF ? q[0] : p[P - 1]) = to_f32<T>(x[HALF ? e + pairs : e + 1]);
+    }
+  };
+  auto turn = [&]() __attribute__((always_inline)) {
     if (c >= turned) {
-      const int e = at + a.rot + (c - turned) * E;
-      float v[E];
-      if constexpr (WIDE) {
-        load16b(x + e, v);
-        store16b(y + e, v);
-      } else {
-        y[e] = x[e];
-      }
+      if constexpr (WIDE) store16b(y + e, p);
+      else y[e] = from_f32<T>(p[0]);
     } else if constexpr (HALF) {
-      const int e = at + c * E;
-      float p[E], q[E];
-      if constexpr (WIDE) {
-        load16b(x + e, p);
-        load16b(x + e + pairs, q);
-      } else {
-        p[0] = to_f32<T>(x[e]);
-        q[0] = to_f32<T>(x[e + pairs]);
-      }
 #pragma unroll
       for (int i = 0; i < E; ++i) {
         const float2 r = cs[c * E + i];
@@ -114,29 +106,37 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
         y[e + pairs] = from_f32<T>(q[0]);
       }
     } else {
-      constexpr int P = WIDE ? E : 2;
-      const int e = at + c * P;
-      float v[P];
-      if constexpr (WIDE) {
-        load16b(x + e, v);
-      } else {
-        v[0] = to_f32<T>(x[e]);
-        v[1] = to_f32<T>(x[e + 1]);
-      }
 #pragma unroll
       for (int i = 0; i < P; i += 2) {
         const float2 r = cs[c * (P / 2) + i / 2];
-        const float b = v[i] * r.y + v[i + 1] * r.x;
-        v[i] = v[i] * r.x - v[i + 1] * r.y;
-        v[i + 1] = b;
+        const float b = p[i] * r.y + p[i + 1] * r.x;
+        p[i] = p[i] * r.x - p[i + 1] * r.y;
+        p[i + 1] = b;
       }
       if constexpr (WIDE) {
-        store16b(y + e, v);
+        store16b(y + e, p);
       } else {
-        y[e] = from_f32<T>(v[0]);
-        y[e + 1] = from_f32<T>(v[1]);
+        y[e] = from_f32<T>(p[0]);
+        y[e + 1] = from_f32<T>(p[1]);
       }
     }
+  };
+  // the first loads are on their way while the sines are formed
+  int u = threadIdx.x;
+  if (u < units) load(u);
+  const int pos = a.pos ? a.pos[row] : (int)row;
+  for (int i = threadIdx.x; i < pairs; i += 256) {
+    double t = (double)pos * a.turns[i];
+    t -= rint(t);
+    float s, c;
+    sincospif(2.0f * (float)t, &s, &c);
+    cs[i] = make_float2(c * a.magnitude, s * a.magnitude);
+  }
+  __syncthreads();
+  while (u < units) {
+    turn();
+    u += 256;
+    if (u < units) load(u);
   }
 }
 
