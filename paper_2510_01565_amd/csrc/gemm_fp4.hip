@@ -75,12 +75,14 @@ __device__ __forceinline__ void asm_mfma_first(f32x16_t& c, const i32x4_t& w, co
   FP4_MFMA_BYTES("=a", "0");
 }
 
-// grouped order: 8 M-tiles share each run of N-tiles, for L2 reuse of both operands.  Groups, which XCDs go through side by
+// grouped order: GM M-tiles share each run of N-tiles, for L2 reuse of both operands.  Groups, which XCDs go through side by
 // side, start an eighth of the N-tiles apart: each part of W then comes from memory at its own time, most of it in the first
 // rounds, and not at the same time for all, who wait for it in every round.  16896 x 16384 x 4096 behind a kernel that
 // reads 256 MB 580 us for 668, 8192^3 277 for 290; with both operands still in the last cache the same.
+// GM 4 for 256x256 tiles, 8 for smaller ones: the first behind the quantising of X 594 us (8: 612, 16: 634); 333 x 4096 x 4096
+// 11.6 us (4: 12.3).
+template <int GM>
 __device__ __forceinline__ void tile_of(int id, int tm, int tn, int& im, int& in) {
-  constexpr int GM = 8;
   const int grp = id / (GM * tn), first = grp * GM, size = min(tm - first, GM), in_grp = id - grp * GM * tn;
   im = first + in_grp % size;
   in = (in_grp / size + grp * max(tn / 8, 1)) % tn;
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(256) void fp4_256_kernel(const Fp4Problem p) {
   };
   auto tile_at = [&](int id, int& m0, int& n0) __attribute__((always_inline)) {
     int im, in;
-    tile_of(id, tm, tn, im, in);
+    tile_of<4>(id, tm, tn, im, in);
     m0 = __builtin_amdgcn_readfirstlane(im * BM);
     n0 = __builtin_amdgcn_readfirstlane(in * BN);
   };
@@ -561,7 +563,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void fp4_ring_kernel(const Fp4Prob
   const int id = (int)(blockIdx.y << kRingRowLog2) + xcd_remap(blockIdx.x, gridDim.x);
   if (id >= tm * tn) return;
   int im, in;
-  tile_of(id, tm, tn, im, in);
+  tile_of<8>(id, tm, tn, im, in);
   const int m0 = im * BM, n0 = in * BN, KT = p.kt, Kp = p.pitch, steps = (KT + KG - 1) / KG;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wv / (WM * WN), wm = wv / WN % WM, wn = wv % WN;
@@ -716,7 +718,7 @@ __global__ __launch_bounds__(NW * 64) void fp4_split_kernel(const Fp4Problem p) 
   const int id = (int)(blockIdx.y << kRingRowLog2) + xcd_remap(blockIdx.x, gridDim.x);
   if (id >= tm * tn) return;
   int im, in;
-  tile_of(id, tm, tn, im, in);
+  tile_of<8>(id, tm, tn, im, in);
   const int m0 = im * BM, n0 = in * BN, Kp = p.pitch;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15, g = lane >> 4;
   char* const lbase = (char*)lds + wv * 2 * TILE;
