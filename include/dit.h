@@ -460,7 +460,8 @@ typedef struct {
  * three may lie in the rows of one fused product.  heads a multiple of kv_heads,
  * heads <= 1024; head_dim 128 or 64 for DIT_BF16, 64 for DIT_F32; precisions as
  * for dit_attention; 2^-64 <= scale <= 2^64.  q, k, v, o 16-byte aligned, strides
- * multiples of 16 bytes and at most 2^22 elements.
+ * multiples of 16 bytes and at most 2^22 elements.  Without queries nothing is done
+ * and every pointer may be NULL; k and v may be where no query's sequence has keys.
  * ws: device workspace of at least dit_attention_grouped_workspace_size() bytes,
  * 256-byte aligned, written by every call: calls that may run at once (two
  * streams, two captured graphs) need one each; it may be NULL where that size is 0.

@@ -1392,14 +1392,25 @@ dit_status dit_attention_grouped(const dit_sequences* seqs, int heads, int kv_he
   if (flags & ~DIT_CAUSAL) return fail(DIT_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
   // positive: the mask's -inf and the running max are of unscaled scores
   if (!(scale >= 0x1p-64f && scale <= 0x1p64f)) return fail(DIT_ERR_INVALID_ARG, "scale %g outside [2^-64, 2^64]", (double)scale);
-  if (!q || !k || !v || !o) return fail(DIT_ERR_INVALID_ARG, "q / k / v / o is NULL");
-  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o))
-    return fail(DIT_ERR_INVALID_ARG, "q / k / v / o must be 16-byte aligned");
   const long qw = (long)heads * head_dim, kw = (long)kv_heads * head_dim, per = 16 / elem_size(dtype);
   if (ldq < qw || ldo < qw || ldkv < kw)
     return fail(DIT_ERR_INVALID_ARG, "ldq %ld or ldo %ld below %ld, or ldkv %ld below %ld", ldq, ldo, qw, ldkv, kw);
   if (ldq % per || ldkv % per || ldo % per) return fail(DIT_ERR_INVALID_ARG, "ldq / ldkv / ldo must be multiples of 16 bytes");
   if (ldq > kMaxRow || ldkv > kMaxRow || ldo > kMaxRow) return fail(DIT_ERR_UNSUPPORTED, "ldq / ldkv / ldo exceeds %d", kMaxRow);
+  a.causal = flags & DIT_CAUSAL;
+  // queries, keys that some query reads, and pairs of both
+  double pairs = 0, rows = 0, keys = 0;
+  for (int i = 0; i < a.n_seq; ++i) {
+    const double n = a.q_len[i], m = n > 0 ? a.kv_len[i] : 0, below = fmax(n - m, 0.0);  // queries that see nothing
+    pairs += a.causal ? (n - below) * (2 * m - (n - below) + 1) / 2 : n * m;
+    rows += n;
+    keys += m;
+  }
+  if (rows == 0) return DIT_OK;
+  if (keys == 0) k = v = q;  // not read; the kernels form addresses from them
+  if (!q || !k || !v || !o) return fail(DIT_ERR_INVALID_ARG, "q / k / v / o is NULL");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o))
+    return fail(DIT_ERR_INVALID_ARG, "q / k / v / o must be 16-byte aligned");
   if (q == o && ldq != ldo) return fail(DIT_ERR_INVALID_ARG, "in place with ldq %ld and ldo %ld", ldq, ldo);
   const size_t need = align256(attention_grouped_bytes(dtype, a));
   if (need && (st = check_ws(ws, ws_bytes, need))) return st;
@@ -1411,15 +1422,7 @@ dit_status dit_attention_grouped(const dit_sequences* seqs, int heads, int kv_he
   a.ldkv = ldkv;
   a.ldo = ldo;
   a.scale = scale;
-  a.causal = flags & DIT_CAUSAL;
   a.part = (float*)ws;
-  double pairs = 0, rows = 0, keys = 0;
-  for (int i = 0; i < a.n_seq; ++i) {
-    const double n = a.q_len[i], m = a.kv_len[i], below = fmax(n - m, 0.0);  // queries that see nothing
-    pairs += a.causal ? (n - below) * (2 * m - (n - below) + 1) / 2 : n * m;
-    rows += n;
-    keys += m;
-  }
   hipStream_t s = (hipStream_t)stream;
   const double bytes = 2.0 * (rows * heads + keys * kv_heads) * head_dim * elem_size(dtype);
   HIP_TRY(timed(s, "attention_grouped", 4.0 * pairs * heads * head_dim, bytes,

@@ -460,3 +460,21 @@ def test_two_layers_at_once_on_two_streams():
         torch.cuda.synchronize()
         for layer, r in zip(layers, want):
             assert torch.equal(layer.o, r)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_queries_without_any_key(dtype, d, causal):
+    """k and v without a row, whose tensors have no address: zeros, for one token as for many."""
+    torch = _torch()
+    dt, code = _dt(dtype)
+    kv = torch.empty((0, 2, 3, d), dtype=dt, device="cuda")
+    for ql, kl, first in (([1], [0], None), ([5, 0, 200], [0, 0, 0], None), ([0, 3], [40, 0], [7, 1 << 20])):
+        seqs = dit.Sequences(ql, kl, first)
+        assert dit.attention_grouped_workspace_size(seqs, 6, 3, d, code) == 0
+        q = torch.full((sum(ql), 6, d), math.nan, dtype=dt, device="cuda")
+        o = torch.full((sum(ql) + 2, 6, d), 3.0, dtype=dt, device="cuda")
+        dit.dit_attention_grouped(seqs, 6, 3, d, code, dit.DIT_CAUSAL if causal else 0, 0.1, q, 6 * d, kv[:, 0], kv[:, 1],
+                                  6 * d, o[1:-1], 6 * d, None, 0)
+        torch.cuda.synchronize()
+        assert (o[0] == 3).all() and (o[-1] == 3).all() and (o[1:-1] == 0).all()

@@ -145,3 +145,25 @@ def test_grouped_refusals():
     assert bad((8, 772)) == BAD and bad((11, 388)) == BAD and bad((13, 388)) == BAD
     assert bad((8, (1 << 22) + 8)) == UNS and bad((11, (1 << 22) + 8)) == UNS and bad((13, (1 << 22) + 8)) == UNS
     assert bad((12, P)) == BAD  # o is q with another stride
+
+
+def test_grouped_without_queries():
+    """Nothing to do, and no pointer needed (that of a tensor without elements is NULL); the rest is checked as ever."""
+    for dtype in (BF, F32):
+        for q in (dit.Sequences([0], [0]), dit.Sequences([0, 0], [3000, 7]), dit.Sequences([0], [5], [9])):
+            assert dit.attention_grouped_workspace_size(q, 6, 3, 64, dtype) == 0
+            ok = [q, 6, 3, 64, dtype, dit.DIT_CAUSAL, 0.125, 0, 384, 0, 0, 192, 0, 384, 0, 0, 0]
+            dit.dit_attention_grouped(*ok)
+            bad = _refusals(dit.dit_attention_grouped, ok)
+            assert bad((2, 4)) == BAD and bad((3, 96)) == UNS and bad((5, 2)) == BAD and bad((6, NAN)) == BAD
+            assert bad((8, 376)) == BAD and bad((11, 184)) == BAD and bad((13, 376)) == BAD and bad((8, (1 << 22) + 8)) == UNS
+
+
+def test_grouped_with_queries_needs_its_pointers():
+    # keys of a sequence without queries are not read: with queries of the other, which has none, k and v may be NULL, q and o may not
+    q = dit.Sequences([0, 3], [40, 0])
+    ok = [q, 6, 3, 64, BF, 0, 0.125, P, 384, 0, 0, 192, P, 384, 0, 0, 0]
+    bad = _refusals(dit.dit_attention_grouped, ok)
+    assert bad((7, 0)) == BAD and bad((12, 0)) == BAD and bad((7, P + 8)) == BAD and bad((12, P + 8)) == BAD
+    for seqs in (dit.Sequences([3], [1]), dit.Sequences([3, 3], [0, 1])):
+        assert bad((0, seqs)) == BAD and bad((0, seqs), (9, P)) == BAD and bad((0, seqs), (10, P)) == BAD
