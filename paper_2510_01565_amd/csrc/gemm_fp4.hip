@@ -10,8 +10,8 @@
 // elements are kept as four words, word j byte i for block 4 i + j: lane l of the
 // smaller form takes word l / 16 for all four steps of 128, of the larger one words
 // l / 32 and l / 32 + 2 for all eight of 64, the byte being a constant of the code.
-// The products of a block are exact, as is the sum of 8 of them; both outputs take
-// the same sums.
+// The products of a block are exact, as is their sum, which meets the other blocks'
+// in fp32; both outputs take the same sums.
 #include <math.h>
 
 #include "device_common.h"

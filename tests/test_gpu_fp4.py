@@ -328,3 +328,47 @@ def test_on_another_stream_and_captured():
             g.replay()
             torch.cuda.synchronize()
             assert torch.equal(y, r), rep
+
+
+@pytest.mark.parametrize("M,N,K,kernel", [
+    (16, 128, 1024, "rows"), (33, 1536, 6144, "16x32"), (128, 1536, 6144, "32x32"), (500, 1536, 1024, "64x64"),
+    (1024, 4096, 1024, "128x128"), (4096, 8192, 1024, "256x256")])
+def test_products_of_a_block_are_summed_exactly(M, N, K, kernel):
+    """Each row one block that makes 2^24, where fp32 has steps of 2, ahead of or behind one whose products are +1 and -1 at
+    random places and come to a positive even number: an output that is exact, which it would not be if fewer than all of a
+    block's products, of which some come to an odd number, were added to the running sum at a time."""
+    torch = _torch()
+    rng = np.random.default_rng(M)
+    blocks = K // 32
+    codes, scales, want = np.zeros((M, K), np.uint8), np.full((M, blocks), 127, np.uint8), np.zeros(M)
+    for m in range(M):
+        big, small = rng.choice(blocks, 2, replace=False)
+        codes[m, big * 32 + rng.integers(32)] = 6                  # 4, times 0.5 and 2^23
+        scales[m, big] = 127 + 23
+        minus = int(rng.integers(0, 8))
+        plus = minus + 2 * int(rng.integers(1, 9))
+        at = small * 32 + rng.permutation(32)[:plus + minus]
+        codes[m, at[:plus]], codes[m, at[plus:]] = 2, 2 | 8       # 1 and -1, times 0.5 and 2
+        scales[m, small] = 128
+        sign = 8 * (m % 2)
+        codes[m][codes[m] > 0] ^= sign
+        want[m] = (2.0 ** 24 + plus - minus) * (-1) ** (m % 2)
+    assert np.array_equal(want, want.astype(np.float32))
+    spread = np.full((M, -(-blocks // 16) * 16), 127, np.uint8)
+    spread[:, :blocks] = scales
+    spread = spread.reshape(M, -1, 4, 4).transpose(0, 1, 3, 2).reshape(M, -1)
+    nc, ns = dit.fp4_layout(M, K)
+    packed = codes[:, 0::2] | codes[:, 1::2] << 4
+    assert packed.size == nc and spread.size == ns
+    xq, xs = (torch.from_numpy(np.ascontiguousarray(a)).cuda() for a in (packed, spread))
+    assert np.array_equal(T.dequantize_fp4(packed, spread, K).sum(1) / 2, want)
+    nc, ns = dit.fp4_layout(N, K)
+    wq = torch.full((nc,), 0x11, dtype=torch.uint8, device="cuda")   # 0.5 everywhere
+    ws = torch.full((ns,), 127, dtype=torch.uint8, device="cuda")
+    y = torch.empty((M, N), dtype=torch.float32, device="cuda")
+    dit.profile_start()
+    dit.dit_linear_fp4(M, N, K, xq, xs, wq, ws, None, dit.DIT_BF16, y, dit.DIT_F32)
+    assert set(dit.profile_stop()) == {"gemm_fp4_" + kernel}
+    want = torch.from_numpy(want).float().cuda()
+    wrong = (y != want[:, None]).nonzero()
+    assert wrong.numel() == 0, (wrong.shape[0], [(int(m), float(y[m, n] - want[m])) for m, n in wrong[:4]])
