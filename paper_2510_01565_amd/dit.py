@@ -315,11 +315,15 @@ def dit_linear_fp4(M: int, N: int, K: int, x_codes, x_scales, w_codes, w_scales,
                                 _ptr(y), out_dtype, _stream(stream)))
 
 
-def rope_frequencies(rot_dim: int, theta: float, factor: float = 1.0, original_len: float = 1.0, low: float = 0.0,
-                     high: float = 0.0):
-    """Host array of rot_dim / 2 angles per position (doubles), for ``dit_rope``."""
+def rope_frequencies(rot_dim: int, theta: float, factor: float = 1.0, original_len: Optional[float] = None,
+                     low: Optional[float] = None, high: Optional[float] = None):
+    """Host array of rot_dim / 2 angles per position (doubles), for ``dit_rope``.  A ``factor`` other than 1 needs the three
+    behind it, which say what pairs it divides."""
+    if factor != 1 and None in (original_len, low, high):
+        raise ValueError(f"factor {factor} needs original_len, low and high")
     w = (ctypes.c_double * max(rot_dim // 2, 1))()
-    _check(lib().dit_rope_frequencies(rot_dim, theta, factor, original_len, low, high, w))
+    _check(lib().dit_rope_frequencies(rot_dim, theta, factor, 1.0 if original_len is None else original_len,
+                                      0.0 if low is None else low, 0.0 if high is None else high, w))
     return w
 
 

@@ -167,3 +167,20 @@ def test_grouped_with_queries_needs_its_pointers():
     assert bad((7, 0)) == BAD and bad((12, 0)) == BAD and bad((7, P + 8)) == BAD and bad((12, P + 8)) == BAD
     for seqs in (dit.Sequences([3], [1]), dit.Sequences([3, 3], [0, 1])):
         assert bad((0, seqs)) == BAD and bad((0, seqs), (9, P)) == BAD and bad((0, seqs), (10, P)) == BAD
+
+
+def test_a_factor_needs_the_context_that_it_extends():
+    """A factor without the length and the limits that say which pairs it divides would leave all frequencies as they are."""
+    for args in ((2.0,), (2.0, 1e5), (2.0, 1e5, 1.0), (NAN,), (0.5,)):
+        with pytest.raises(ValueError):
+            dit.rope_frequencies(8, 1e4, *args)
+    for kw in ({"low": 1.0, "high": 4.0}, {"original_len": 1e5, "high": 4.0}, {"original_len": 1e5, "low": 1.0}):
+        with pytest.raises(ValueError):
+            dit.rope_frequencies(8, 1e4, factor=8.0, **kw)
+    plain = list(dit.rope_frequencies(8, 1e4))
+    assert plain == list(dit.rope_frequencies(8, 1e4, 1.0)) == list(dit.rope_frequencies(8, 1e4, 1.0, 4096.0, 1.0, 4.0))
+    assert plain == list(dit.rope_frequencies(8, 1e4, original_len=4096.0)) == list(dit.rope_frequencies(8, 1e4, low=1.0, high=4.0))
+    assert list(dit.rope_frequencies(8, 1e4, 8.0, 1e5, low=0.0, high=0.0)) == plain  # asked for: every pair turns 0 times or more
+    # limits that are given are checked without a factor too
+    assert _err(dit.rope_frequencies, 8, 1e4, 1.0, 4096.0, 4.0, 1.0) == BAD
+    assert _err(lambda: dit.rope_frequencies(8, 1e4, low=-1.0)) == BAD and _err(lambda: dit.rope_frequencies(8, 1e4, original_len=0.0)) == BAD
