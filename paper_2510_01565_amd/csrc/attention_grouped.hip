@@ -791,8 +791,9 @@ void grouped_few_kernel(const GroupedArgs a) {
 
 // ---------------------------------------------------------------- ranges of keys joined
 // A row's ranges in their order; `t` of the HD / 4 threads that take 4 dimensions each.  FEW: tiles of kFewRows rows, one to
-// a sequence, whose ranges may be many: a block takes one row (`rows` to a sequence, what the longest has: kFewRows cost 3 of
-// 57 us where each has four), and its 8 groups of threads every 8th range each, which meet in LDS.  Otherwise the block of a tile's first range takes the tile, 8 rows at a time.
+// a sequence, whose ranges may be many: a block takes one row, and its 8 groups of threads every 8th range each, which meet
+// in LDS.  `rows` blocks to a sequence, as many as the longest has rows: kFewRows cost 3 of 57 us where each has four.
+// Otherwise the block of a tile's first range takes the tile, 8 rows at a time.
 struct Joined {
   float m, l;
   float4 y;
@@ -877,7 +878,7 @@ struct Plan {
 enum Kind { ROWS, FEW, F32 };
 
 // The sequences of `in` that `kind` takes, cut into ranges where the launch is then modelled to end sooner.
-constexpr size_t kMostBytes = 128 << 20;
+constexpr size_t kMostBytes = 128 << 20;  // of partial results: a launch that would need more is not cut
 Plan plan_of(const GroupedArgs& in, Kind kind, bool may_cut = true) {
   Plan p;
   p.a = in;
@@ -939,14 +940,8 @@ void launch_merge(const Plan& p, hipStream_t s) {
 
 }  // namespace
 
-size_t attention_grouped_bytes(int dtype, const GroupedArgs& in) {
-  size_t most = 0;
-  GroupedArgs a = in;
-  for (a.causal = 0; a.causal < 2; ++a.causal) {
-    if (dtype == DIT_F32) most = std::max(most, plan_of(a, F32).bytes);
-    else most = std::max(most, std::max(plan_of(a, FEW).bytes, plan_of(a, ROWS).bytes));
-  }
-  return most;
+size_t attention_grouped_bytes(int dtype, const GroupedArgs& a) {
+  return dtype == DIT_F32 ? plan_of(a, F32).bytes : std::max(plan_of(a, FEW).bytes, plan_of(a, ROWS).bytes);
 }
 
 hipError_t launch_attention_grouped(int dtype, const GroupedArgs& a, hipStream_t s) {

@@ -328,13 +328,14 @@ struct GroupedArgs {
   int q_len[DIT_MAX_SEQUENCES];
   int kv_len[DIT_MAX_SEQUENCES];
   long kv_row[DIT_MAX_SEQUENCES];  // first row of k and v
-  // Set by the launcher.  Row tiles of the sequences before, a tile's key ranges counted one by one; a sequence of more than
-  // `chunk` keys is cut into ranges of `chunk`, whose partial results go to `part` and are merged by a second kernel.
+  // Set by the launcher.  Row tiles of the sequences before, a tile's key ranges counted one by one; the keys of a tile that
+  // sees more than `chunk` are cut into even ranges of at most that many (but for whole key tiles), whose partial results go
+  // to `part` and are merged by a second kernel.
   int tile_off[DIT_MAX_SEQUENCES + 1];
   int chunk;
   float* part;
 };
-// bytes of `part` that any launch of these sequences needs, causal or not
+// bytes of `part` that a launch of these sequences needs, the same causal or not
 size_t attention_grouped_bytes(int dtype, const GroupedArgs& a);
 hipError_t launch_attention_grouped(int dtype, const GroupedArgs& a, hipStream_t s);
 
