@@ -465,10 +465,14 @@ typedef struct {
  * ws: device workspace of at least dit_attention_grouped_workspace_size() bytes,
  * 256-byte aligned, written by every call: calls that may run at once (two
  * streams, two captured graphs) need one each; it may be NULL where that size is 0.
+ * The size is that of these very lengths: longer ones may need less, so a program
+ * whose lengths grow asks ahead of each call or keeps 128 MiB, the most there is.
  * It holds the partial results of launches with few query tiles, whose keys are cut
  * into ranges and merged in a fixed order: outputs repeat bit for bit, but their
  * order of sums follows from the whole batch.  o may be q itself with ldo = ldq;
  * otherwise it may not overlap q, k or v.
+ * A captured graph keeps the lengths, rows and cuts of the call that was captured:
+ * one more token of each sequence is another call, and another capture.
  */
 #define DIT_CAUSAL 1
 dit_status dit_attention_grouped_workspace_size(const dit_sequences* seqs, int heads, int kv_heads, int head_dim, int dtype,

@@ -1,5 +1,7 @@
 """Layouts, frequencies and refusals of the 4-bit products, the rotary positions and the grouped attention: every call
 here returns on the host, none reaches the GPU."""
+import random
+
 import pytest
 
 from paper_2510_01565_amd import dit
@@ -184,3 +186,21 @@ def test_a_factor_needs_the_context_that_it_extends():
     # limits that are given are checked without a factor too
     assert _err(dit.rope_frequencies, 8, 1e4, 1.0, 4096.0, 4.0, 1.0) == BAD
     assert _err(lambda: dit.rope_frequencies(8, 1e4, low=-1.0)) == BAD and _err(lambda: dit.rope_frequencies(8, 1e4, original_len=0.0)) == BAD
+
+
+def test_grouped_workspace_is_of_these_lengths_and_bounded():
+    size = dit.attention_grouped_workspace_size
+    # one token over a cache of 32 / 8 heads of 128: ranges of 256 keys up to 16384, evenly longer ones from there on.  A
+    # range of a key head holds 32 rows of 128 sums, a maximum and a sum.
+    for keys, ranges in ((768, 0), (769, 4), (4096, 16), (16384, 64), (16385, 65), (16448, 52), (65536, 64), (1 << 24, 64)):
+        assert size(dit.Sequences([1], [keys]), 32, 8, 128, BF) == ranges * 8 * 32 * 130 * 4, keys
+    rng = random.Random(3)
+    most = 0
+    for _ in range(400):
+        kv_heads = rng.choice([1, 2, 8, 32, 64, 128, 1024])
+        heads = kv_heads * rng.choice([g for g in (1, 2, 8, 64) if g * kv_heads <= 1024])
+        kv = [int(2 ** rng.uniform(0, 24)) for _ in range(rng.choice([1, 3, 30, 128]))]
+        q = [min(m, int(2 ** rng.uniform(0, rng.choice([1, 6, 16])))) for m in kv]
+        for d, dtype in ((64, BF), (128, BF), (64, F32)):
+            most = max(most, size(dit.Sequences(q, kv), heads, kv_heads, d, dtype))
+    assert 64 << 20 < most <= 128 << 20
