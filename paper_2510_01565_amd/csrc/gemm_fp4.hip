@@ -445,8 +445,11 @@ __global__ __launch_bounds__(256) void fp4_256_kernel(const Fp4Problem p) {
   using P2 = std::integral_constant<int, 2>;
   using P3 = std::integral_constant<int, 3>;
   // Blocks that finish a tile at the same time write at the same time, and wait for it.  An XCD's 32 blocks start up to 6 us
-  // apart where a block has several tiles of short K to win that back: behind the quantising of X 16896 x 8192 x 2048 takes
-  // 196 us for 206, 16896 x 16384 x 1024 242 for 256, 16717 x 6144 x 1536 135 for 136; but 16896 x 16384 x 4096 617 for 609.
+  // apart where a block has several tiles of short K to win that back.  Quantising of X and product, in us, with it and with
+  // the same code that starts at once: 16717 x 6144 x 1536 139 and 141, in fp32 160 and 169; 16717 x 6144 x 2048 166 and 167;
+  // 16896 x 8192 x 2048 207 and 210; 16896 x 16384 x 1024 256 and 264; 24000 x 16384 x 800 348 and 358; 8192 x 16384 x 1024
+  // 132 and 136, in fp32 x 2048 214 both; 20000 x 5000 x 1800 218 both; but 16384 x 6144 x 768, just six tiles a block, 105
+  // and 102.  A card with faster memory gains half as much.  16896 x 16384 x 4096 617 and 609, and so long K starts at once.
   if (KT <= kStaggerKTiles && tiles >= kStaggerRounds * kMaxBlocks256)
     for (int i = (int)blockIdx.x >> 3; i > 0; --i) __builtin_amdgcn_s_sleep(6);
   // as 8 phases ahead of the first would have: those that load tile 0's and 1's places
