@@ -110,11 +110,13 @@ __device__ __forceinline__ float2* part_ml(const GroupedArgs& a, int id, int per
 // into two stages; V is transposed on its way from LDS to the matrix cores.
 // 16384 tokens of 32 heads of 128, causal, 1.9 ms, 1.15 PFLOP/s; without the softmax
 // 1.64, without P V 1.23: matrix and vector instructions both, at the clock that the
-// power leaves.  Twelve prompts of 1 to 4096 tokens, 24 heads of 64, 88 us: here the
-// vector instructions, six issues a score, four of them its exponential's.  Slower
-// were two groups of waves that take turns at the two (2.12 ms: a wave alone on a SIMD
-// issues vector instructions at half the rate of two), and a max that is looked at
-// ahead of the exponentials (1.93 ms).
+// power leaves.  Twelve prompts of 1 to 4096 tokens, 24 heads of 64, 88 us, 0.8
+// PFLOP/s: here the matrix cores are busy 34% of the time and the vector units, six
+// issues a score, 49%.  A tile's scores, exponentials and products with V wait for each
+// other, a barrier ends it, and 2.1 waves a SIMD, the launch's end counted in, are all
+// there is to fill in.  Slower were two groups of waves that take turns at the two
+// (2.12 ms: a wave alone on a SIMD issues vector instructions at half the rate of two),
+// and a max that is looked at ahead of the exponentials (1.93 ms).
 template <int HD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2)))
 void grouped_bf16_kernel(const GroupedArgs a) {
@@ -378,8 +380,10 @@ void grouped_bf16_kernel(const GroupedArgs a) {
 // merged at the end in wave order.  K and V go straight from memory to registers, in
 // 16-byte pieces: a lane's piece of V holds 4 neighbouring dimensions of a key, each a
 // row of another MFMA.  The next tile's K replaces this one's once the scores are done,
-// its V once O is.  Sixteen sequences of 1 to 16384 keys, 258 MB, 64 us, 4.1 TB/s; rows
-// of prompts are bound by the fp32 matrix instructions.
+// its V once O is.  Sixteen sequences of 1 to 16384 keys, 258 MB, 64 us, 4.1 TB/s.  The
+// twelve prompts, 24 heads, 860 us, 82 TFLOP/s of the 157 that the matrix cores have:
+// these are busy 53% of the time, the vector units 47%: the products, softmax and
+// rescaled sums of 16 keys depend on each other, and 2.8 waves share a SIMD.
 constexpr int FD = 64, FQ = 16;
 
 __global__ __launch_bounds__(256) void grouped_f32_kernel(const GroupedArgs a) {
@@ -913,7 +917,9 @@ Plan plan_of(const GroupedArgs& in, Kind kind, bool may_cut = true) {
   const int least = kind == ROWS ? 1024 : 256, whole = kind == ROWS ? 2048 : 768;
   double even = fmax(keys / 512 * (kind == ROWS ? 2 : 1), least);
   // Many rows: no more than 256 blocks in the end (300 queries over 4096 keys 62 us, one range more to a tile 72), and no more
-  // than 8 ranges of a tile, which one block joins (64 over 16384 69 us, 16 ranges 76, 4 ranges 87).
+  // than 8 ranges of a tile, which one block joins (64 over 16384 69 us, 16 ranges 76, 4 ranges 87).  That is of 8 key heads;
+  // fewer leave CUs idle: 33 rows and more of one tile and one key head are 8 blocks, a token of 40 heads to one key head over
+  // 65536 keys 135 us, of 32, which the kernel for few rows takes, 20.
   if (kind == ROWS) even = fmax(longest / fmin(fmax(floor(longest / even), 1.0), 8.0), least);
   a.chunk = !may_cut || longest <= whole || even >= longest ? kWhole : ((int)even + kKeys - 1) / kKeys * kKeys;
   a.tile_off[0] = 0;
